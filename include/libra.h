@@ -131,6 +131,23 @@ int libra_plan_tiles(const int32_t* cu_seqlens_dev, int n_samples, int n_heads, 
                      const libra_plan_opts* opts /* nullable */, void* stream,
                      libra_plan_t** plan_out);
 
+/* The same for attention with a sliding window and sinks (no counterpart in the paper, whose layers attend to all of a
+ * sample's past): a query at position p of its sample attends the keys at positions k <= p with
+ *     p - k < window   or   k < sinks,
+ * that is the last `window` positions, its own among them, and the first `sinks` of its sample.  The plan carries the
+ * mask: libra_attn_pool_fwd, libra_attn_pool_bwd, libra_attn_pool_bwd_noalloc and libra_attn_pool_bwd_ckpt8 called with it
+ * compute attention and gradients over those pairs, in every form and at every head_dim; key blocks that no row of a tile
+ * sees are not read.  Tile weights count the visible pairs (LIBRA_WEIGHT_PAIRS) or the executed blocks
+ * (LIBRA_WEIGHT_BLOCKS); the pair-blocks of a query chunk are the key blocks of which it sees a key: with sinks those that
+ * hold the sinks of its first row's sample, then the others, ascending.
+ * A window that is not below T, or not below any sample's length, gives what libra_plan_tiles gives.  As there, an infinity or
+ * a NaN of a key or value reaches rows that do not see it where they share a 128-row block with rows, and a key
+ * block with keys, that are seen.
+ * Errors: INVALID_ARG (window < 1, sinks < 0), otherwise those of libra_plan_tiles. */
+int libra_plan_tiles_window(const int32_t* cu_seqlens_dev, int n_samples, int n_heads, int tile_q,
+                            const libra_plan_opts* opts /* nullable */, int window, int sinks, void* stream,
+                            libra_plan_t** plan_out);
+
 /* Sizes of a plan direction (host values, no synchronisation). */
 int libra_plan_info(const libra_plan_t* plan, int direction, int64_t* n_tiles, int* n_workers,
                     int64_t* n_blocks, int* tile, int* n_heads);
@@ -181,7 +198,7 @@ int libra_plan_destroy(libra_plan_t* plan);
  * mask of Section 2.3):  for row i of a sample starting at s, with keys s..i,
  *     out_i = sum_k softmax_k(scale * <q_i, k_k>) v_k,   lse_i = ln sum_k exp(scale * <q_i, k_k>)
  * bf16 inputs, fp32 accumulation and softmax, bf16 out (round to nearest even), fp32 lse
- * (natural log).  One persistent kernel walks the plan's query-major tile lists.  head_dim 256 (the
+ * (natural log).  (With a plan of libra_plan_tiles_window the keys are those of its mask.)  One persistent kernel walks the plan's query-major tile lists.  head_dim 256 (the
  * micro-benchmark head shape of Table 1) runs a kernel of its own: 256 rows on a pair of CTAs against
  * 64-key blocks, the 256-column output accumulator taking half of the tensor memory.
  * Requires a plan with LIBRA_DIR_Q, tile_q == 256 and n_heads dividing hq.

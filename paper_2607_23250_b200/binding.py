@@ -26,7 +26,7 @@ ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_PLAN_MISMATCH, ERR_CUDA = -1, -2, -3, -4
 ERR_OVERFLOW, ERR_TIMEOUT, ERR_BAD_SEQLENS, ERR_NO_DEVICE = -5, -6, -7, -8
 ERR_SCRATCH_TOO_SMALL = -9
 
-EXPORTS = ["libra_plan_tiles", "libra_plan_info", "libra_plan_status", "libra_plan_export",
+EXPORTS = ["libra_plan_tiles", "libra_plan_tiles_window", "libra_plan_info", "libra_plan_status", "libra_plan_export",
            "libra_plan_export_pairs", "libra_plan_fused_ctas", "libra_plan_destroy", "libra_attn_pool_fwd", "libra_attn_pool_bwd_workspace_bytes",
            "libra_attn_pool_bwd", "libra_attn_pool_bwd_noalloc_max_bytes", "libra_attn_pool_bwd_noalloc",
            "libra_tap_schedule", "libra_busy_times", "libra_tile_times", "libra_plan_set_wait_limit_ns", "libra_plan_inject_stall", "libra_plan_set_timing", "libra_kernel_time_ms", "libra_kernel_times_ms", "libra_selftest_wait_timeout", "libra_launch_count",
@@ -182,11 +182,19 @@ class Plan:
 def libra_plan_tiles(cu_seqlens: torch.Tensor, n_heads: int, tile_q: int, n_workers: int = 0,
                      directions: int = 0, tile_kv: int = 0, n_heads_kv: int = 0, total_tokens: int = 0,
                      stream=None, weight_model: int = 0, cost_block: int = 0, unit_cost_q: int = 0,
-                     unit_cost_kv: int = 0, pair_chunk: int = 0) -> Plan:
+                     unit_cost_kv: int = 0, pair_chunk: int = 0, window: int = 0, sinks: int = 0) -> Plan:
+    """window > 0: a query sees the last `window` positions of its sample, its own among them, and the sample's first
+    `sinks` (libra_plan_tiles_window); 0: all of its sample's past."""
     assert cu_seqlens.is_cuda and cu_seqlens.dtype == torch.int32 and cu_seqlens.is_contiguous()
     opts = PlanOpts(n_workers, directions, tile_kv, n_heads_kv, total_tokens, weight_model, cost_block,
                     unit_cost_q, unit_cost_kv, pair_chunk)
     h = _vp()
+    if window != 0 or sinks != 0:
+        _check(_lib.libra_plan_tiles_window(_ptr(cu_seqlens), ctypes.c_int(cu_seqlens.numel() - 1), ctypes.c_int(n_heads),
+                                            ctypes.c_int(tile_q), ctypes.byref(opts), ctypes.c_int(window),
+                                            ctypes.c_int(sinks), _stream(stream), ctypes.byref(h)),
+               "libra_plan_tiles_window")
+        return Plan(h, cu_seqlens)
     _check(_lib.libra_plan_tiles(_ptr(cu_seqlens), ctypes.c_int(cu_seqlens.numel() - 1), ctypes.c_int(n_heads),
                                  ctypes.c_int(tile_q), ctypes.byref(opts), _stream(stream), ctypes.byref(h)),
            "libra_plan_tiles")

@@ -77,6 +77,8 @@ struct DkvParams {
     const int32_t* cta_offsets;
     const int32_t* cta_tiles;
     const int32_t* tok_end;
+    const int32_t* blk_end;  // [ceil(T / 128)] largest tok_end of a block's keys, and a bound of them from below
+    const int32_t* blk_min;
     int64_t T, Tpad;
     int hq, hkv;
     float scale, scale_log2;
@@ -87,11 +89,9 @@ struct DkvParams {
     uint64_t* busy;
 };
 
-// Query blocks a key block [k0, k0+128) is seen by: diagonal .. block of (end of last key's sample - 1).
-__device__ __forceinline__ int last_q_block(const int32_t* tok_end, int64_t T, int64_t k0) {
-    const int64_t last_key = (k0 + kBlk <= T ? k0 + kBlk : T) - 1;
-    return (tok_end[last_key] - 1) / kBlk;
-}
+// Query blocks a key block [k0, k0+128) is seen by: diagonal .. block of the last query that sees one of its keys (without a
+// window and sinks the last one of its last key's sample).
+__device__ __forceinline__ int last_q_block(const int32_t* blk_end, int64_t k0) { return (blk_end[k0 / kBlk] - 1) / kBlk; }
 
 __device__ __forceinline__ void tmem_ld128(uint32_t taddr, uint32_t* r) {
     tmem_ld32(taddr, r);
@@ -278,7 +278,7 @@ k_attn_bwd_dkdv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 const int kvh = t % p.hkv;
                 const int64_t k0 = (int64_t)(t / p.hkv) * kBlk;
                 const int i_lo = (int)(k0 / kBlk);
-                const int nblk = last_q_block(p.tok_end, p.T, k0) - i_lo + 1;
+                const int nblk = last_q_block(p.blk_end, k0) - i_lo + 1;
                 const int it0 = SHARE ? share_begin(G * nblk, rank, size) : 0;
                 const int n_it = (SHARE ? share_begin(G * nblk, rank + 1, size) : G * nblk) - it0;
                 if (SHARE && n_it == 0) break;
@@ -365,7 +365,7 @@ k_attn_bwd_dkdv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 const int t = p.cta_tiles[idx];
                 const int64_t k0 = (int64_t)(t / p.hkv) * kBlk;
                 const int i_lo = (int)(k0 / kBlk);
-                const int nblk = last_q_block(p.tok_end, p.T, k0) - i_lo + 1;
+                const int nblk = last_q_block(p.blk_end, k0) - i_lo + 1;
                 const int n_it = SHARE ? share_begin(G * nblk, rank + 1, size) - share_begin(G * nblk, rank, size) : G * nblk;
                 if (SHARE && n_it == 0) break;
                 ok = mbar_wait(bar_kvfull, ucnt & 1, abort_flag);
@@ -437,7 +437,7 @@ k_attn_bwd_dkdv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             const int t = p.cta_tiles[idx];
             const int64_t k0 = (int64_t)(t / p.hkv) * kBlk;
             const int i_lo = (int)(k0 / kBlk);
-            const int nblk = last_q_block(p.tok_end, p.T, k0) - i_lo + 1;
+            const int nblk = last_q_block(p.blk_end, k0) - i_lo + 1;
             const int n_it = SHARE ? share_begin(G * nblk, rank + 1, size) - share_begin(G * nblk, rank, size) : G * nblk;
             // ---- dS group: dS^T = P^T o (dP^T - D) ----
             for (int it = 0; it < n_it && ok; ++it, ++it_all) {
@@ -517,7 +517,7 @@ k_attn_bwd_dkdv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             const int kvh = t % p.hkv;
             const int64_t k0 = (int64_t)(t / p.hkv) * kBlk;
             const int i_lo = (int)(k0 / kBlk);
-            const int nblk = last_q_block(p.tok_end, p.T, k0) - i_lo + 1;
+            const int nblk = last_q_block(p.blk_end, k0) - i_lo + 1;
             const int it0 = SHARE ? share_begin(G * nblk, rank, size) : 0;
             const int n_it = (SHARE ? share_begin(G * nblk, rank + 1, size) : G * nblk) - it0;
             const int64_t key = k0 + r;
@@ -526,7 +526,7 @@ k_attn_bwd_dkdv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             const int c0 = 64 * grp;   // this group's query columns
             const uint64_t scale2 = f2_pack(p.scale_log2, p.scale_log2), neg1 = f2_pack(-1.f, -1.f);
             const int kend = key_ok ? p.tok_end[key] : 0;
-            const int min_kend = p.tok_end[k0];
+            const int min_kend = p.blk_min[k0 / kBlk];
             const bool partial = k0 + kBlk > p.T;
             for (int it = 0; it < n_it && ok; ++it, ++it_all) {
                 const int qb = (i_lo + (it0 + it) % nblk) * kBlk;
@@ -764,10 +764,12 @@ static int launch_bwd(const CUtensorMap& tq, const CUtensorMap& tk, const CUtens
     if (!cfg_done(kSlot)) {   // per device
         if (set_smem(k_attn_bwd_dkdv<D, false>, DkvSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
         if (set_smem(k_attn_bwd_dkdv<D, true>, DkvSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
-        if (set_smem(k_attn_bwd_dq<D>, DqSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
+        if (set_smem(k_attn_bwd_dq<D, false>, DqSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
+        if (set_smem(k_attn_bwd_dq<D, true>, DqSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
         if (!regs_pool_ok(k_attn_bwd_dkdv<D, false>, 128, kDkvRegsDs, 128, kDkvRegsOther)) return LIBRA_ERR_UNSUPPORTED;
         if (!regs_pool_ok(k_attn_bwd_dkdv<D, true>, 128, kDkvRegsDs, 128, kDkvRegsOther)) return LIBRA_ERR_UNSUPPORTED;
-        if (!regs_pool_ok(k_attn_bwd_dq<D>, 128 * kDqGroups, kDqRegsCompute, 128, kDqRegsOther)) return LIBRA_ERR_UNSUPPORTED;
+        if (!regs_pool_ok(k_attn_bwd_dq<D, false>, 128 * kDqGroups, kDqRegsCompute, 128, kDqRegsOther)) return LIBRA_ERR_UNSUPPORTED;
+        if (!regs_pool_ok(k_attn_bwd_dq<D, true>, 128 * kDqGroups, kDqRegsCompute, 128, kDqRegsOther)) return LIBRA_ERR_UNSUPPORTED;
         cfg_mark(kSlot);
     }
     time_begin(mp, 1, s);
@@ -785,7 +787,8 @@ static int launch_bwd(const CUtensorMap& tq, const CUtensorMap& tk, const CUtens
     time_end(mp, 1, s);
     time_begin(mp, 2, s);
     if (e == cudaSuccess)
-        e = launch_dependent(k_attn_bwd_dq<D>, Wb, kDqThreads, DqSmem<D>::kBytes, s, tq, tk, tv, tdo, tdq, pb);
+        e = launch_dependent(mp->sinks ? k_attn_bwd_dq<D, true> : k_attn_bwd_dq<D, false>, Wb, kDqThreads, DqSmem<D>::kBytes, s, tq, tk,
+                             tv, tdo, tdq, pb);
     time_end(mp, 2, s);
     count_launch(2);
     return e == cudaSuccess ? LIBRA_OK : LIBRA_ERR_CUDA;
@@ -869,6 +872,7 @@ static int launch_fused(const void* q_dev, const void* k_dev, const void* v_dev,
         pp.lse2 = lse2; pp.dvec = dvec;
         pp.cta_offsets = wide.d_cta_offsets; pp.cta_tiles = wide.d_cta_exec;
         pp.u_blk = wide.d_u_blk; pp.u_chunk = wide.d_u_chunk; pp.tok_end = plan->d_tok_end;
+        pp.blk_end = plan->d_blk_end; pp.blk_min = plan->d_blk_min;
         pp.T = T; pp.Tpad = ws.Tpad; pp.NU = (int)wide.NB;
         pp.hq = dims->hq; pp.hkv = dims->hkv; pp.R = wide.chunk / kBlk;
         pp.scale_log2 = scale * 1.4426950408889634f;
@@ -876,6 +880,7 @@ static int launch_fused(const void* q_dev, const void* k_dev, const void* v_dev,
         pp.wait_limit_ns = plan->wait_limit_ns; pp.inject_stall = plan->inject_stall;
         pp.busy = d.d_busy;
         pp.tile_ns = d.d_tile_ns; pp.first_j = d.d_first_j; pp.base = d.d_base; pp.NU128 = d.NB;
+        pp.sink_j = d.d_sink_j; pp.sink_n = d.d_sink_n;
         mp->n_outcome[1] = 2 * wide.W;
         time_begin(mp, 4, s);
         e = launch_dependent(k_attn_bwd_pair, 2 * wide.W, kPairThreads, PairSmem::kBytes, s, tq, tk, tv, tdo, tq64, tdo64, tacc, tdkacc,
@@ -896,6 +901,7 @@ static int launch_fused(const void* q_dev, const void* k_dev, const void* v_dev,
         fp.lse2 = lse2; fp.dvec = dvec;
         fp.cta_offsets = d.d_cta_offsets; fp.cta_tiles = d.d_cta_exec;
         fp.u_blk = d.d_u_blk; fp.u_chunk = d.d_u_chunk; fp.tok_end = plan->d_tok_end;
+        fp.blk_end = plan->d_blk_end; fp.blk_min = plan->d_blk_min;
         fp.T = T; fp.Tpad = ws.Tpad; fp.NU = d.NB;
         fp.hq = dims->hq; fp.hkv = dims->hkv; fp.R = d.chunk / d.tile;
         fp.scale_log2 = scale * 1.4426950408889634f;
@@ -1015,6 +1021,8 @@ extern "C" int libra_attn_pool_bwd(const void* q_dev, const void* k_dev, const v
     pa.cta_offsets = dkv_dir.d_cta_offsets;
     pa.cta_tiles = dkv_dir.d_cta_exec;
     pa.tok_end = plan->d_tok_end;
+    pa.blk_end = plan->d_blk_end;
+    pa.blk_min = plan->d_blk_min;
     pa.T = T;
     pa.Tpad = ws.Tpad;
     pa.hq = dims->hq;
@@ -1033,6 +1041,8 @@ extern "C" int libra_attn_pool_bwd(const void* q_dev, const void* k_dev, const v
     pb.cta_offsets = dq_dir.d_cta_offsets;
     pb.cta_tiles = dq_dir.d_cta_exec;
     pb.tok_start = plan->d_tok_start;
+    pb.tok_first = plan->d_tok_first;
+    pb.sinks = plan->sinks;
     pb.T = T;
     pb.Tpad = ws.Tpad;
     pb.hq = dims->hq;
@@ -1049,7 +1059,9 @@ extern "C" int libra_attn_pool_bwd(const void* q_dev, const void* k_dev, const v
     // Several CTAs a dK/dV tile when there are that many for each (the first NT workers then have one tile each) and a key
     // block's samples give every one of them a few iterations on average.  Not with one query head per kv head: the dQ tiles
     // are as long then (2000 tokens, 4 / 4 heads of 64: step 53.1 us without, 54.8 with two).
-    const int64_t its = (int64_t)(dims->hq / dims->hkv) * (T / plan->n) / kBlk;
+    int64_t reach = T / plan->n;   // rows that see a key block, on average
+    if (plan->window && reach > plan->window + kBlk) reach = plan->window + kBlk;
+    const int64_t its = (int64_t)(dims->hq / dims->hkv) * reach / kBlk;
     int share = dims->hq > dims->hkv ? 8 : 1;
     while (share > 1 && (share * dkv_dir.NT > dkv_dir.W || 2 * share > its)) share /= 2;
     libra_plan_t* mp = const_cast<libra_plan_t*>(plan);

@@ -52,8 +52,10 @@ struct DqParams {
     const int32_t* cta_offsets;
     const int32_t* cta_tiles;
     const int32_t* tok_start;
+    const int32_t* tok_first;   // SINK: first token of the row's sample
     int64_t T, Tpad;
     int hq, hkv, H;
+    int sinks;
     float scale, scale_log2;
     int* outcome;
     int side_by_side;        // start without waiting for the dK/dV kernel
@@ -65,11 +67,17 @@ struct DqParams {
 
 // Walks the units of one CTA in the order every role uses: tiles of the CTA's list x the two 128-row
 // sub-blocks of a tile x the heads of the shard.  A sub-block past the end of the pool is skipped.
+template <bool SINK>
 struct DqUnit {
     int64_t q0;
     int lo, hi, h;  // key blocks lo..hi, query head h
+    int slo, shi;   // SINK: and, ahead of them, slo..shi < lo, which hold the sinks of the first row's sample
     bool valid;
+    __device__ __forceinline__ int first() const { return SINK && slo <= shi ? slo : lo; }
+    __device__ __forceinline__ int after(int j) const { return SINK && j == shi ? lo : j + 1; }
+    __device__ __forceinline__ int count() const { return hi - lo + 1 + (SINK && slo <= shi ? shi - slo + 1 : 0); }
 };
+template <bool SINK>
 struct DqUnitIter {
     const DqParams& p;
     int idx, end, sub, hh, hps;
@@ -78,8 +86,8 @@ struct DqUnitIter {
         : p(p_), idx(begin), end(end_), sub(0), hh(0), hps(heads_per_shard) {
         t = idx < end ? p.cta_tiles[idx] : 0;
     }
-    __device__ DqUnit next() {
-        DqUnit u;
+    __device__ DqUnit<SINK> next() {
+        DqUnit<SINK> u;
         u.valid = false;
         while (idx < end) {
             const int64_t q0 = (int64_t)(t / p.H) * (2 * kBlk) + sub * kBlk;
@@ -88,6 +96,13 @@ struct DqUnitIter {
                 u.q0 = q0;
                 u.lo = p.tok_start[q0] / kBlk;
                 u.hi = (int)(q0 / kBlk);
+                if (SINK) {
+                    const int first = p.tok_first[q0];
+                    const int64_t end = (int64_t)first + p.sinks;
+                    u.slo = first / kBlk;
+                    u.shi = min((int)((end < p.T ? end : p.T) - 1) / kBlk, u.lo - 1);
+                    if (u.shi < u.slo) u.shi = -1;
+                }
                 u.h = (t % p.H) * hps + hh;
                 u.valid = true;
             }
@@ -105,7 +120,7 @@ struct DqUnitIter {
     }
 };
 
-template <int D>
+template <int D, bool SINK>
 __global__ void __launch_bounds__(kDqThreads, 1)
 k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
               const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_do,
@@ -209,8 +224,8 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         // cycles per unit.
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDqRegsOther));
         if (elect_one()) {
-            DqUnitIter units(p, tile_begin, tile_end, heads_per_shard);
-            DqUnit u = units.next();
+            DqUnitIter<SINK> units(p, tile_begin, tile_end, heads_per_shard);
+            DqUnit<SINK> u = units.next();
             uint32_t cnt = 0;
             bool ok = true;
             if (u.valid) {  // first unit: its Q rows have been copied to TMEM, the tile may be reloaded
@@ -239,13 +254,13 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             uint32_t ucnt = 0, kcnt = 0, vcnt = 0;
             uint32_t n_q = 0, n_do = 0;   // Q / dO loads armed so far (for the give-up path)
             bool ok = true;
-            DqUnitIter units(p, tile_begin, tile_end, heads_per_shard);
-            DqUnit u = units.next();
+            DqUnitIter<SINK> units(p, tile_begin, tile_end, heads_per_shard);
+            DqUnit<SINK> u = units.next();
             // Q and dO of unit `un`, whose tiles go through phase `cnt` of their barriers.  The shared-memory
             // copies are free again as soon as the compute groups have moved the previous unit's rows into
             // TMEM, which happens at the end of the unit before it: the next unit's Q and dO (first touches,
             // DRAM latency) can therefore be requested a whole unit ahead.
-            auto load_q_do = [&](const DqUnit& un, uint32_t cnt) -> bool {
+            auto load_q_do = [&](const DqUnit<SINK>& un, uint32_t cnt) -> bool {
                 if (!mbar_wait(bar_qempty, (cnt & 1) ^ 1, abort_flag)) return false;
                 mbar_arrive_expect_tx(bar_qfull, L::kTileBytes);
                 ++n_q;
@@ -261,11 +276,11 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             if (p.inject_stall) u.valid = false;   // test aid: no loads at all
             if (u.valid) ok = load_q_do(u, 0);
             while (u.valid && ok) {
-                const DqUnit nx = units.next();
-                const int h = u.h, kvh = h / G, lo = u.lo, hi = u.hi;
-                const int j_q = lo + 1 < hi ? lo + 1 : hi;  // after this block's K/V the next unit's Q / dO are requested
+                const DqUnit<SINK> nx = units.next();
+                const int h = u.h, kvh = h / G, first = u.first(), hi = u.hi;
+                const int second = u.after(first), j_q = second < hi ? second : hi;  // after this block's K/V the next unit's Q / dO are requested
                 ++ucnt;
-                for (int j = lo; j <= hi && ok; ++j) {
+                for (int j = first; j <= hi && ok; j = u.after(j)) {
                     const uint32_t ks = kcnt % L::kKStages;
                     ok = mbar_wait(&bar_kempty[ks], ((kcnt / L::kKStages) & 1) ^ 1, abort_flag);
                     if (!ok) break;
@@ -291,7 +306,8 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                         if (!ok) break;
                         // pull the next unit's first K / V blocks into L2 meanwhile: the rings hold one block of lead, which
                         // covers an L2 hit but not a first touch in DRAM
-                        for (int jj = nx.lo; jj <= nx.hi && jj < nx.lo + 2; ++jj)
+                        const int ahead = nx.after(nx.first());
+                        for (int jj = nx.first(); jj <= nx.hi && jj <= ahead; jj = nx.after(jj))
                             for (int half = 0; half < D / 64; ++half) {
                                 tma_prefetch_3d(&tm_k, half * 64, nx.h / G, jj * kBlk);
                                 tma_prefetch_3d(&tm_v, half * 64, nx.h / G, jj * kBlk);
@@ -351,8 +367,8 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                 ++vcnt;
                 return true;
             };
-            DqUnitIter units(p, tile_begin, tile_end, heads_per_shard);
-            DqUnit u = units.next();
+            DqUnitIter<SINK> units(p, tile_begin, tile_end, heads_per_shard);
+            DqUnit<SINK> u = units.next();
             uint32_t ucnt = 0;
             if (u.valid) {  // first unit: nothing to overlap its first S and dP with
                 ok = mbar_wait(bar_qtready, 0, abort_flag);
@@ -361,32 +377,32 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                 if (ok) { tc_fence_after(); ok = do_dp(); }
             }
             while (u.valid && ok) {
-                const DqUnit nx = units.next();
-                const int lo = u.lo, hi = u.hi;
-                const uint32_t kbase = kcnt;  // ring index of K_lo
-                for (int j = lo; j <= hi && ok; ++j, ++blk) {
-                    const bool last = j == hi;
+                const DqUnit<SINK> nx = units.next();
+                const int n = u.count();
+                const uint32_t kbase = kcnt;  // ring index of the first block's K
+                for (int i = 0; i < n && ok; ++i, ++blk) {
+                    const bool last = i == n - 1;
                     // S(j+1) as soon as the compute groups have read S(j)
                     if (!last) {
                         ok = mbar_wait(bar_sfree, blk & 1, abort_flag);
                         if (!ok) break;
                         tc_fence_after();
-                        ok = do_s(kbase + (j + 1 - lo));
+                        ok = do_s(kbase + i + 1);
                         if (!ok) break;
                     }
                     // dQ += dS(j) K_j
                     ok = mbar_wait(bar_dsready, blk & 1, abort_flag);
-                    if (ok && j == lo && ucnt > 0) ok = mbar_wait(bar_dqempty, (ucnt - 1) & 1, abort_flag);  // dQ read out
+                    if (ok && i == 0 && ucnt > 0) ok = mbar_wait(bar_dqempty, (ucnt - 1) & 1, abort_flag);  // dQ read out
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t kidx = kbase + (j - lo);
+                    const uint32_t kidx = kbase + i;
                     {
                         const uint64_t ka = sdesc_advance(mdesc0, L::kKOff + (kidx % L::kKStages) * L::kTileBytes);
 #pragma unroll
                         for (int kk = 0; kk < 8; ++kk)  // 16 keys per step; group c left dS of its keys at columns CW c ..
                             mma_ts(tmem_base + kColDQ,
                                    tmem_base + kColDP + (kk / (kDqCW / 16)) * kDqCW + (kk % (kDqCW / 16)) * 8,
-                                   sdesc_advance(ka, kk * 2048), idesc_dq, (j > lo || kk > 0) ? 1u : 0u);
+                                   sdesc_advance(ka, kk * 2048), idesc_dq, (i > 0 || kk > 0) ? 1u : 0u);
                         tc_commit(&bar_kempty[kidx % L::kKStages]);
                         if (last) tc_commit(bar_dqfull);
                     }
@@ -399,14 +415,14 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                         if (ok) ok = mbar_wait(bar_qtready, (ucnt + 1) & 1, abort_flag);
                         if (!ok) break;
                         tc_fence_after();
-                        ok = do_s(kbase + (hi - lo + 1));
+                        ok = do_s(kbase + n);
                         if (ok) ok = mbar_wait(bar_dotready, (ucnt + 1) & 1, abort_flag);
                         if (!ok) break;
                         tc_fence_after();
                         ok = do_dp();
                     }
                 }
-                kcnt = kbase + (hi - lo + 1);
+                kcnt = kbase + n;
                 ++ucnt;
                 u = nx;
             }
@@ -454,21 +470,28 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         struct RowCtx {
             float lse2, dsum;
             int kstart, max_kstart;
+            int sink_lo, sink_hi;   // SINK: the row's sinks ahead of its window
             bool row_ok;
         };
-        auto load_ctx = [&](const DqUnit& un) {
+        auto load_ctx = [&](const DqUnit<SINK>& un) {
             RowCtx x;
             const int64_t row = un.q0 + r;
             x.row_ok = row < p.T;
             x.kstart = x.row_ok ? p.tok_start[row] : 0;
             const int64_t last_row = (un.q0 + kBlk <= p.T ? un.q0 + kBlk : p.T) - 1;
             x.max_kstart = p.tok_start[last_row];
+            x.sink_lo = 0;
+            x.sink_hi = -1;
+            if (SINK && x.row_ok) {
+                x.sink_lo = p.tok_first[row];
+                x.sink_hi = (int)min((int64_t)x.sink_lo + p.sinks, (int64_t)x.kstart) - 1;
+            }
             x.lse2 = p.lse2[(size_t)un.h * p.Tpad + row];  // padded rows hold zeros
             x.dsum = p.dvec[(size_t)un.h * p.Tpad + row];
             return x;
         };
-        DqUnitIter units(p, tile_begin, tile_end, heads_per_shard);
-        DqUnit u = units.next();
+        DqUnitIter<SINK> units(p, tile_begin, tile_end, heads_per_shard);
+        DqUnit<SINK> u = units.next();
         RowCtx cx{};
         if (u.valid) {
             cx = load_ctx(u);
@@ -476,15 +499,15 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             mbar_arrive(bar_dqstaged);   // phase 0: the store thread frees the Q tile once every row has been read
         }
         while (u.valid && ok) {
-            const DqUnit nx = units.next();
+            const DqUnit<SINK> nx = units.next();
             RowCtx cx_next{};
             if (nx.valid) cx_next = load_ctx(nx);
-            const int lo = u.lo, hi = u.hi;
+            const int first = u.first(), hi = u.hi;
             const int64_t row = u.q0 + r;
             const bool row_ok = cx.row_ok;
             const int kstart = cx.kstart, max_kstart = cx.max_kstart;
             const float lse2 = cx.lse2, dsum = cx.dsum;
-            for (int j = lo; j <= hi && ok; ++j, ++blk) {
+            for (int j = first; j <= hi && ok; j = u.after(j), ++blk) {
                 const int k0 = j * kBlk;
                 const bool need_mask = (j == hi) || (k0 < max_kstart) || !row_ok;
                 const int c_lo = (row_ok ? kstart - k0 : kBlk) - CW * c;    // first visible column of this group's range
@@ -508,7 +531,8 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                 if (need_mask) {
 #pragma unroll
                     for (int w = 0; w < CW / 32; ++w) {
-                        const uint32_t vis = range_bits(c_lo - 32 * w, c_hi - 32 * w);
+                        uint32_t vis = range_bits(c_lo - 32 * w, c_hi - 32 * w);
+                        if (SINK) vis |= range_bits(cx.sink_lo - k0 - CW * c - 32 * w, cx.sink_hi - k0 - CW * c - 32 * w);
 #pragma unroll
                         for (int i = 0; i < 32; ++i) pf[32 * w + i] = (vis >> i) & 1u ? pf[32 * w + i] : 0.f;
                     }

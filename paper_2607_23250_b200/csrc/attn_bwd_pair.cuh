@@ -90,6 +90,8 @@ struct PairParams {
     const int32_t* u_blk;     // 256-key block of wide pair-block u
     const int32_t* u_chunk;   // query chunk of it
     const int32_t* tok_end;
+    const int32_t* blk_end;   // of a 128-key block's keys the largest tok_end, and a bound from below
+    const int32_t* blk_min;
     int64_t T, Tpad;
     int NU;                   // wide pair-blocks
     int hq, hkv, R;           // R = row blocks per query chunk
@@ -99,26 +101,34 @@ struct PairParams {
     uint32_t wait_limit_ns;
     int inject_stall;         // test aid: the odd CTAs' producers issue no loads
     uint64_t* busy;
-    // times by 128-key pair tiles, the halves of the wide ones (same chunks): tile h NU128 + base[c] + j - first_j[c]
+    // times by 128-key pair tiles, the halves of the wide ones (same chunks): tile h NU128 + base[c] + j - first_j[c]; with
+    // sinks the sink_n[c] blocks from sink_j[c] come first (null without)
     uint32_t* tile_ns;
     const int32_t* first_j;
     const int64_t* base;
+    const int32_t* sink_j;
+    const int32_t* sink_n;
     int64_t NU128;
+    // tile of a head for key block j of chunk c
+    __device__ __forceinline__ int64_t tile128(int c, int j) const {
+        const int n = sink_n ? sink_n[c] : 0;
+        return base[c] + (j < first_j[c] ? j - (n ? sink_j[c] : 0) : n + j - first_j[c]);
+    }
 };
 
 // The row blocks [i0, i0 + n_blk) that a wide pair tile walks for every head of its group.
 struct PairUnit {
     int kvh, c, j0, i0, n_blk;
-    int last0;                // last row block that sees the lower key block
+    int last0, last1;         // last row blocks that see the lower and the upper key block (sinks: in either order)
     bool two;                 // the upper key block exists
     // row blocks of it that see key block j0 + r
     __device__ __forceinline__ int seen(uint32_t r) const {
         const int end = i0 + n_blk;
         if (r == 0) return (last0 < end ? last0 + 1 : end) - i0;
-        return two ? end - (i0 > j0 ? i0 : j0 + 1) : 0;
+        return two ? (last1 < end ? last1 + 1 : end) - (i0 > j0 ? i0 : j0 + 1) : 0;
     }
     // bit r: row block i sees key block j0 + r
-    __device__ __forceinline__ uint32_t see(int i) const { return (i <= last0 ? 1u : 0u) | (two && i > j0 ? 2u : 0u); }
+    __device__ __forceinline__ uint32_t see(int i) const { return (i <= last0 ? 1u : 0u) | (two && i > j0 && i <= last1 ? 2u : 0u); }
 };
 __device__ __forceinline__ PairUnit pair_unit(const PairParams& p, int t) {
     PairUnit u;
@@ -127,9 +137,10 @@ __device__ __forceinline__ PairUnit pair_unit(const PairParams& p, int t) {
     u.j0 = 2 * p.u_blk[pb];
     u.c = p.u_chunk[pb];
     const int64_t k1 = (int64_t)(u.j0 + 1) * kBlk;
-    u.last0 = last_q_block(p.tok_end, p.T, (int64_t)u.j0 * kBlk);
+    u.last0 = last_q_block(p.blk_end, (int64_t)u.j0 * kBlk);
     u.two = k1 < p.T;
-    const int last = u.two ? last_q_block(p.tok_end, p.T, k1) : u.last0;
+    u.last1 = u.two ? last_q_block(p.blk_end, k1) : u.last0;
+    const int last = u.last1 > u.last0 ? u.last1 : u.last0;
     const int lo = u.c * p.R > u.j0 ? u.c * p.R : u.j0;
     const int hi = u.c * p.R + p.R - 1 < last ? u.c * p.R + p.R - 1 : last;
     u.i0 = lo;
@@ -576,7 +587,7 @@ k_attn_bwd_pair(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             const int64_t k0 = (int64_t)(u.j0 + rank) * kBlk, key = k0 + r;
             const bool key_ok = key < p.T;
             const int kend = key_ok ? p.tok_end[key] : 0;
-            const int min_kend = k0 < p.T ? p.tok_end[k0] : 0;
+            const int min_kend = k0 < p.T ? p.blk_min[k0 / kBlk] : 0;
             const bool partial = k0 + kBlk > p.T;
             for (int it = 0, i = 0; it < n_it && ok; ++it, ++n) {
                 const int qb = (u.i0 + i) * kBlk;
@@ -656,7 +667,7 @@ k_attn_bwd_pair(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             __syncwarp();
             if (lane < 2) mbar_arrive_cluster(map_to_rank(&bars[L::kDkvEmpty], (uint32_t)lane));
             if (threadIdx.x == 0 && seen > 0)   // of the time of both halves the part in which this one had work
-                p.tile_ns[u.kvh * p.NU128 + p.base[u.c] + u.j0 + rank - p.first_j[u.c]] = (uint32_t)((globaltimer_ns() - tile_t0) * seen / u.n_blk);
+                p.tile_ns[u.kvh * p.NU128 + p.tile128(u.c, u.j0 + (int)rank)] = (uint32_t)((globaltimer_ns() - tile_t0) * seen / u.n_blk);
         }
         // every bulk reduce this warp issued has completed before the CTA leaves
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");

@@ -104,6 +104,9 @@ struct Params {
     const int32_t* cta_tiles;
     const int32_t* tok_start;
     const int32_t* tok_end;
+    const int32_t* blk_end; // [ceil(T / 128)] largest tok_end of a block's keys
+    const int32_t* tok_first;   // SINK: first token of the row's sample
+    int sinks;
     int64_t T, Tpad;
     int hq, hkv, H;         // H: head shards of the query-major lists (FWD, DQ)
     int W;                  // FWD, DQ: workers of the lists; a pair of CTAs runs the lists of two
@@ -127,16 +130,18 @@ struct Params {
 //   key-stationary passes: one unit per tile of the pair's list (256 keys x one kv head); its iterations are the query
 //   heads of the group times the 64-row query blocks from the diagonal to the end of the last key's sample (of the chunk);
 //   query-stationary passes: a query-major tile (256 rows x head shard) of the lists of two workers gives one unit per
-//   head; its iterations are the 64-key blocks from the start of the first row's sample to the diagonal.
+//   head; its iterations are the 64-key blocks from the first key that the first row's window holds to the diagonal.  SINK:
+//   ahead of them the blocks below that hold the sinks of the first row's sample.
 // r0 is the first of this CTA's 128 stationary rows.
-template <int MODE>
+template <int MODE, bool SINK>
 struct Units {
     static constexpr bool kKeys = Cfg<MODE>::kKeyStationary;
     const Params& p;
     int idx, end, hh, hps, G;
     int64_t base, r0;       // first stationary row of the pair and of this CTA
     int h, kvh, b_lo, n_blk, n_it;
-    int bound0, bound1;     // of each CTA's rows: start of the first one's sample (queries), end of the last one's (keys)
+    int bound0, bound1;     // of each CTA's rows: first key that the first one's window holds (queries), end of the queries that see one (keys)
+    int early, early_lo;    // SINK: blocks ahead of the window's, the first of them
     __device__ Units(const Params& p_, int cta) : p(p_) {
         const int c = cta >> 1;
         if (kKeys) {
@@ -158,9 +163,9 @@ struct Units {
             const int j = p.acc32 ? p.u_blk[(int)(t % p.NU)] : t / p.hkv;
             kvh = p.acc32 ? (int)(t / p.NU) : t % p.hkv;
             base = (int64_t)j * (2 * kRows);
-            bound0 = p.tok_end[base + kRows - 1 < p.T ? base + kRows - 1 : p.T - 1];
-            bound1 = p.tok_end[base + 2 * kRows - 1 < p.T ? base + 2 * kRows - 1 : p.T - 1];
-            int last64 = (bound1 - 1) / kBlk;
+            bound0 = p.blk_end[base / kRows];
+            bound1 = base + kRows < p.T ? p.blk_end[base / kRows + 1] : bound0;
+            int last64 = ((bound1 > bound0 ? bound1 : bound0) - 1) / kBlk;
             b_lo = (int)(base / kBlk);
             if (p.acc32) {   // pair tile: the query blocks of one chunk only
                 const int c = p.u_chunk[(int)(t % p.NU)], lo64 = 2 * c * p.R, hi64 = 2 * (c * p.R + p.R) - 1;
@@ -178,10 +183,35 @@ struct Units {
             kvh = h / G;
             b_lo = bound0 / kBlk;
             n_blk = (int)(last_row / kBlk) - b_lo + 1;
+            if constexpr (SINK) {
+                const int first = p.tok_first[base];
+                early_lo = first / kBlk;
+                early = min(sink_block(first), b_lo - 1) - early_lo + 1;
+                if (early < 0) early = 0;
+                n_blk += early;
+            }
             n_it = n_blk;
         }
         r0 = base + rank * kRows;
         return true;
+    }
+    // Last block that holds a sink of a sample starting at `first`.
+    __device__ __forceinline__ int sink_block(int first) const {
+        const int64_t e = (int64_t)first + p.sinks;
+        return (int)((e < p.T ? e : p.T) - 1) / kBlk;
+    }
+    // SINK: the blocks that hold sinks which CTA c's first row sees ahead of its window, of the unit's 0 .. n_blk - 1 (the
+    // other rows see no more of them, or have samples that start among the CTA's rows).
+    __device__ void early_by(uint32_t c, int& lo, int& hi) const {
+        const int64_t a = base + c * kRows;
+        lo = 0;
+        hi = -1;
+        if (a >= p.T) return;
+        const int first = p.tok_first[a], start = p.tok_start[a], b0 = first / kBlk;
+        if (first >= start) return;
+        const int b1 = min(sink_block(first), start / kBlk);
+        lo = b0 < b_lo ? b0 - early_lo : early + b0 - b_lo;
+        hi = b1 < b_lo ? b1 - early_lo : early + b1 - b_lo;
     }
     // Streamed blocks of a head that some row of CTA c sees: [lo, hi], of the unit's 0 .. n_blk - 1 (lo > hi: none).
     __device__ void seen_by(uint32_t c, int& lo, int& hi) const {
@@ -190,13 +220,20 @@ struct Units {
         lo = kKeys ? (int)(a / kBlk) : bound / kBlk;
         hi = kKeys ? (bound - 1) / kBlk : (int)(z / kBlk);
         lo = lo > b_lo ? lo - b_lo : 0;
+        if constexpr (SINK) {
+            lo += early;
+            hi += early;
+        }
         hi = a >= p.T ? -1 : (hi - b_lo < n_blk ? hi - b_lo : n_blk - 1);
     }
     // First row of the streamed block j of a head; the iterations of a unit take its heads in turn, blocks ascending.
-    __device__ int stream_row(int j) const { return (b_lo + j) * kBlk; }
+    __device__ int stream_row(int j) const {
+        if constexpr (SINK) return (j < early ? early_lo + j : b_lo + j - early) * kBlk;
+        return (b_lo + j) * kBlk;
+    }
 };
 
-template <int MODE>
+template <int MODE, bool SINK>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 k_attn_d256(const __grid_constant__ CUtensorMap tm_sa, const __grid_constant__ CUtensorMap tm_sb,
             const __grid_constant__ CUtensorMap tm_t0, const __grid_constant__ CUtensorMap tm_t1,
@@ -287,7 +324,7 @@ k_attn_d256(const __grid_constant__ CUtensorMap tm_sa, const __grid_constant__ C
     if (warp == kTmaWarp) {
         // ---------------- TMA producer (each CTA loads its own halves; the leader's barriers count both) ----------------
         if (elect_one()) {
-            Units<MODE> u(p, cta);
+            Units<MODE, SINK> u(p, cta);
             uint32_t n = 0, uc = 0;          // n: iterations so far (over all units)
             uint32_t tiles = 0;
             bool ok = true;
@@ -356,7 +393,7 @@ k_attn_d256(const __grid_constant__ CUtensorMap tm_sa, const __grid_constant__ C
                     mma_ss_pair(tmem_base + d_col, sdesc_advance(da, (kk / 4) * L::kBigHalf + (kk % 4) * 32),
                                 sdesc_advance(db, (kk / 4) * L::kRowHalf + (kk % 4) * 32), idesc_x, kk > 0);
             };
-            Units<MODE> u(p, cta);
+            Units<MODE, SINK> u(p, cta);
             uint32_t uc = 0, itc = 0;
             uint32_t xi = 0, xb = 0;   // next block to multiply, its X1 buffer
             bool ok = true;
@@ -394,6 +431,11 @@ k_attn_d256(const __grid_constant__ CUtensorMap tm_sa, const __grid_constant__ C
                 int lo0, hi0, lo1, hi1, j = 0;
                 u.seen_by(0, lo0, hi0);
                 u.seen_by(1, lo1, hi1);
+                int elo0 = 0, ehi0 = -1, elo1 = 0, ehi1 = -1;
+                if constexpr (SINK) {
+                    u.early_by(0, elo0, ehi0);
+                    u.early_by(1, elo1, ehi1);
+                }
                 uint32_t begun = 0;              // bit per CTA: its rows of the unit's accumulator have been written
                 for (int it = 0; it < u.n_it && ok; ++it, ++itc) {
                     const uint32_t s = itc % S, ph = (itc / S) & 1, b = itc & 1;
@@ -401,7 +443,8 @@ k_attn_d256(const __grid_constant__ CUtensorMap tm_sa, const __grid_constant__ C
                     // before W of the previous block was ready, and its accumulating GEMM, which may read W there, is ahead
                     // of them in the pipe.
                     if (it + kAhead < u.n_it) ok = do_x(it + kAhead == u.n_it - 1);
-                    const uint32_t see = (j >= lo0 && j <= hi0 ? 1u : 0u) | (j >= lo1 && j <= hi1 ? 2u : 0u);
+                    uint32_t see = (j >= lo0 && j <= hi0 ? 1u : 0u) | (j >= lo1 && j <= hi1 ? 2u : 0u);
+                    if (SINK) see |= (j >= elo0 && j <= ehi0 ? 1u : 0u) | (j >= elo1 && j <= ehi1 ? 2u : 0u);
                     const bool plain = see == 3 && (begun == 0 || begun == 3);
                     if (++j == u.n_blk) j = 0;
                     if (ok) ok = mbar_wait(&bar_full[L::kAcc * S + s], ph, abort_flag);
@@ -454,7 +497,7 @@ k_attn_d256(const __grid_constant__ CUtensorMap tm_sa, const __grid_constant__ C
         const uint32_t t_base = tmem_base + lane_addr;
         const uint32_t t_acc = t_base + kColAcc + grp * (kD / L::kGroups);
         const uint32_t wready0 = map_to_rank(bar_wready, 0), accfree0 = map_to_rank(bar_accfree, 0);
-        Units<MODE> u(p, cta);
+        Units<MODE, SINK> u(p, cta);
         uint32_t uc = 0, itc = 0;
         uint32_t xb = 0, xph = 0;                    // X1 buffer of the block and its phase
         uint32_t lb = 0;                             // FWD: the unit's slot of row sums
@@ -472,6 +515,11 @@ k_attn_d256(const __grid_constant__ CUtensorMap tm_sa, const __grid_constant__ C
             } else {
                 lo_abs = row_ok ? p.tok_start[row] : 0;
                 hi_abs = row_ok ? (int)row : -1;
+            }
+            int sink_lo = 0, sink_hi = -1;           // SINK: the row's sinks ahead of its window
+            if (SINK && row_ok) {
+                sink_lo = p.tok_first[row] - col0;
+                sink_hi = (int)min((int64_t)p.tok_first[row] + p.sinks, (int64_t)p.tok_start[row]) - 1 - col0;
             }
             lo_abs -= col0;                          // counted from this thread's first column
             hi_abs -= col0;
@@ -510,7 +558,8 @@ k_attn_d256(const __grid_constant__ CUtensorMap tm_sa, const __grid_constant__ C
                     if (need_mask) {
 #pragma unroll
                         for (int w = 0; w < kBlk / 32; ++w) {
-                            const uint32_t vis = range_bits(c_lo - 32 * w, c_hi - 32 * w);
+                            uint32_t vis = range_bits(c_lo - 32 * w, c_hi - 32 * w);
+                            if (SINK) vis |= range_bits(sink_lo - b0 - 32 * w, sink_hi - b0 - 32 * w);
 #pragma unroll
                             for (int i = 0; i < 32; ++i) sr[32 * w + i] = (vis >> i) & 1u ? sr[32 * w + i] : 0xff800000u;  // -inf
                         }
@@ -585,7 +634,8 @@ k_attn_d256(const __grid_constant__ CUtensorMap tm_sa, const __grid_constant__ C
                     }
                     if (need_mask) {
                         static_assert(MODE == FWD || NC == 32, "one mask word per compute thread");
-                        const uint32_t vis = range_bits(c_lo, c_hi);
+                        uint32_t vis = range_bits(c_lo, c_hi);
+                        if (SINK) vis |= range_bits(sink_lo - b0, sink_hi - b0);
 #pragma unroll
                         for (int i = 0; i < NC; ++i) pf[i] = (vis >> i) & 1u ? pf[i] : 0.f;
                     }
@@ -697,7 +747,7 @@ k_attn_d256(const __grid_constant__ CUtensorMap tm_sa, const __grid_constant__ C
         const int w = warp - 4;
         const uint32_t t_acc = tmem_base + ((uint32_t)(w * 32) << 16) + kColAcc;
         const uint32_t accfree0 = map_to_rank(bar_accfree, 0);
-        Units<MODE> u(p, cta);
+        Units<MODE, SINK> u(p, cta);
         uint32_t uc = 0, lb = 0, lph = 0;
         while (u.next(rank)) {
             if (!warp_wait(bar_accdone, uc & 1, abort_flag) || !warp_wait(&bar_lfull[lb], lph, abort_flag)) break;
@@ -780,20 +830,21 @@ k_attn_d256(const __grid_constant__ CUtensorMap tm_sa, const __grid_constant__ C
     if (MODE == DK || MODE == DQ) grid_dep_wait();
 }
 
-template <int MODE>
+template <int MODE, bool SINK>
 static int launch(const CUtensorMap& sa, const CUtensorMap& sb, const CUtensorMap& t0, const CUtensorMap& t1, const CUtensorMap& t2,
                   const Params& prm, int W, libra_plan* mp, cudaStream_t s) {
     using L = Cfg<MODE>;
-    if (!cfg_done(8 + MODE)) {   // per device
-        if (cudaFuncSetAttribute(k_attn_d256<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes) != cudaSuccess)
+    constexpr int kSlot = 8 + MODE + (SINK ? 6 : 0);
+    if (!cfg_done(kSlot)) {   // per device
+        if (cudaFuncSetAttribute(k_attn_d256<MODE, SINK>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes) != cudaSuccess)
             return LIBRA_ERR_CUDA;
-        cfg_mark(8 + MODE);
+        cfg_mark(kSlot);
     }
     count_launch();
     const unsigned grid = 2 * ((W + 1) / 2);   // a pair of CTAs for every two workers
     mp->n_outcome[MODE] = (int)grid;
-    return launch_dependent(k_attn_d256<MODE>, grid, kThreads, L::kBytes, s, sa, sb, t0, t1, t2, prm) == cudaSuccess ? LIBRA_OK
-                                                                                                                : LIBRA_ERR_CUDA;
+    return launch_dependent(k_attn_d256<MODE, SINK>, grid, kThreads, L::kBytes, s, sa, sb, t0, t1, t2, prm) == cudaSuccess
+               ? LIBRA_OK : LIBRA_ERR_CUDA;
 }
 
 }  // namespace d256
@@ -815,6 +866,9 @@ int launch_fwd_d256(const void* q, const void* k, const void* v, void* out, floa
     prm.cta_tiles = d.d_cta_exec;
     prm.tok_start = plan->d_tok_start;
     prm.tok_end = plan->d_tok_end;
+    prm.blk_end = plan->d_blk_end;
+    prm.tok_first = plan->d_tok_first;
+    prm.sinks = plan->sinks;
     prm.T = plan->T;
     prm.Tpad = (plan->T + 127) / 128 * 128;
     prm.hq = dims->hq; prm.hkv = dims->hkv; prm.H = d.H; prm.W = d.W;
@@ -822,7 +876,8 @@ int launch_fwd_d256(const void* q, const void* k, const void* v, void* out, floa
     prm.outcome = plan->d_outcome[0]; prm.plan_status = plan->d_status;
     prm.wait_limit_ns = plan->wait_limit_ns; prm.inject_stall = plan->inject_stall;
     prm.busy = d.d_busy;
-    return launch<FWD>(tq, tq, tk, tv, to, prm, d.W, const_cast<libra_plan*>(plan), s);
+    libra_plan* mp = const_cast<libra_plan*>(plan);
+    return plan->sinks ? launch<FWD, true>(tq, tq, tk, tv, to, prm, d.W, mp, s) : launch<FWD, false>(tq, tq, tk, tv, to, prm, d.W, mp, s);
 }
 
 // Backward at head_dim 256: the dV and dK passes over the key-major lists, the dQ pass over the query-major lists.
@@ -853,6 +908,9 @@ int launch_bwd_d256(const void* q, const void* k, const void* v, const void* dou
     prm.lse2 = lse2; prm.dvec = dvec;
     prm.tok_start = plan->d_tok_start;
     prm.tok_end = plan->d_tok_end;
+    prm.blk_end = plan->d_blk_end;
+    prm.tok_first = plan->d_tok_first;
+    prm.sinks = plan->sinks;
     prm.T = plan->T;
     prm.Tpad = Tpad;
     prm.hq = dims->hq; prm.hkv = dims->hkv; prm.H = dq_dir.H; prm.W = dq_dir.W;
@@ -866,13 +924,13 @@ int launch_bwd_d256(const void* q, const void* k, const void* v, const void* dou
     time_begin(mp, 1, s);
     prm.out = reinterpret_cast<__nv_bfloat16*>(dv);
     prm.acc32 = dv_acc;
-    rc = launch<DV>(k128, k128, q32, do64, do64, prm, plan->W, mp, s);
+    rc = launch<DV, false>(k128, k128, q32, do64, do64, prm, plan->W, mp, s);
     prm.out = reinterpret_cast<__nv_bfloat16*>(dk);
     prm.acc32 = dk_acc;
     prm.outcome = plan->d_outcome[2];
     prm.side_by_side = side_by_side(kv_dir.NT, kv_dir.W);
     prm.busy = plan->dir[pairs ? 2 : 1].d_busy;
-    if (rc == LIBRA_OK) rc = launch<DK>(k128, v128, q32, do32, q64, prm, plan->W, mp, s);
+    if (rc == LIBRA_OK) rc = launch<DK, false>(k128, v128, q32, do32, q64, prm, plan->W, mp, s);
     time_end(mp, 1, s);
     prm.acc32 = nullptr;
     if (rc != LIBRA_OK) return rc;
@@ -882,7 +940,8 @@ int launch_bwd_d256(const void* q, const void* k, const void* v, const void* dou
     prm.outcome = plan->d_outcome[3];
     if (dq_in_place(dq, q, dout, dims)) prm.side_by_side = 0;
     time_begin(mp, 2, s);
-    rc = launch<DQ>(q128, do128, k32, v32, k64, prm, dq_dir.W, mp, s);
+    rc = plan->sinks ? launch<DQ, true>(q128, do128, k32, v32, k64, prm, dq_dir.W, mp, s)
+                     : launch<DQ, false>(q128, do128, k32, v32, k64, prm, dq_dir.W, mp, s);
     time_end(mp, 2, s);
     return rc;
 }

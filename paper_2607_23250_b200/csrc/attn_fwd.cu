@@ -6,6 +6,9 @@
 // holds the start of the first row's sample.  Blocks are cut at multiples of 128 on the
 // pool's token axis, so the diagonal block of a sub-tile is aligned with it and every other
 // visible block is either dense or needs the per-row sample-start mask.
+// A window moves the first key of a row (tok_start) closer and changes nothing else: it never decreases from row to row, like
+// the start of a sample.  With sinks (SINK) a slot goes through a second run of blocks, those that hold the sinks of its
+// first row's sample and lie ahead of its window, after the others; a masked block's visible columns are then two ranges.
 //
 // Roles (384 threads): warps 0-3 and 4-7 are the softmax groups of slot 0 and 1 (one row per
 // thread, S read from TMEM, P written back to TMEM as bf16 over S), warp 8 issues TMA loads,
@@ -65,8 +68,10 @@ struct FwdParams {
     const int32_t* cta_offsets;
     const int32_t* cta_tiles;
     const int32_t* tok_start;
+    const int32_t* tok_first;  // SINK: first token of the row's sample
     int64_t T;
     int hq, hkv, H;
+    int sinks;
     float scale_log2;  // softmax scale * log2(e)
     int* outcome;      // [gridDim.x] 0 or what kept this CTA from doing its work
     const int* plan_status;  // the planner's verdict on cu_seqlens: non-zero = do not run
@@ -77,10 +82,23 @@ struct FwdParams {
 };
 
 // One tile of the CTA's list: id, first row, key blocks lo[g] .. hi[g] of slot g (lo > hi: the slot lies past T).
+// SINK: also blocks slo[g] .. shi[g] < lo[g].  What slot 1 sees lies among slot 1's diagonal block and what slot 0 sees: its
+// first row's sample is slot 0's, or starts in slot 0.
+template <bool SINK>
 struct FwdTile {
     int t;
     int64_t q0;
     int lo[2], hi[2];
+    int slo[SINK ? 2 : 1], shi[SINK ? 2 : 1];
+    // The walk of the tile, downwards: the block after j, of slot g (0: of the tile), -1 at the end (SINK only).
+    __device__ __forceinline__ int after(int j, int g) const {
+        if (j == (j >= lo[g] ? lo[g] : slo[g])) return j >= lo[g] && shi[g] >= slo[g] ? shi[g] : -1;
+        return j - 1;
+    }
+    __device__ __forceinline__ int last() const { return SINK && shi[0] >= slo[0] ? slo[0] : lo[0]; }
+    __device__ __forceinline__ bool sees(int g, int j) const {
+        return (j >= lo[g] && j <= hi[g]) || (SINK && j >= slo[g] && j <= shi[g]);
+    }
     // A tile that a pair of CTAs shares: `shared`, and part[g] when both have key blocks of slot g.
     bool shared, part[2];
     // Takes the CTA's part: rank 0 the upper half of the key blocks, rank 1 the lower; false when nothing is left for it.
@@ -101,11 +119,14 @@ struct FwdTile {
 };
 // Walks the list.  Ids are fetched two tiles and sample starts one tile ahead: a chain of two dependent global
 // loads between tiles would leave the tensor pipe idle for about 2000 clk.
+template <bool SINK>
 struct FwdTiles {
     const FwdParams& p;
     int idx, end;
     int t1, t2, a1, b1;   // next tile: id, tok_start of the first row of each slot; id of the one after
-    __device__ __forceinline__ FwdTiles(const FwdParams& p_, int begin, int end_) : p(p_), idx(begin), end(end_), a1(0), b1(0) {
+    int a0, b0;           // SINK: the same rows' tok_first
+    __device__ __forceinline__ FwdTiles(const FwdParams& p_, int begin, int end_)
+        : p(p_), idx(begin), end(end_), a1(0), b1(0), a0(0), b0(0) {
         t1 = idx < end ? p.cta_tiles[idx] : -1;
         t2 = idx + 1 < end ? p.cta_tiles[idx + 1] : -1;
         fetch();
@@ -115,8 +136,17 @@ struct FwdTiles {
         const int64_t q0 = (int64_t)(t1 / p.H) * (2 * kBM);
         a1 = p.tok_start[q0];
         b1 = q0 + kBM < p.T ? p.tok_start[q0 + kBM] : 0;
+        if (SINK) {
+            a0 = p.tok_first[q0];
+            b0 = q0 + kBM < p.T ? p.tok_first[q0 + kBM] : 0;
+        }
     }
-    __device__ __forceinline__ bool next(FwdTile& x) {
+    // Last block that holds a sink of a sample starting at `first`.
+    __device__ __forceinline__ int sink_block(int first) const {
+        const int64_t end = (int64_t)first + p.sinks;
+        return (int)((end < p.T ? end : p.T) - 1) / kBN;
+    }
+    __device__ __forceinline__ bool next(FwdTile<SINK>& x) {
         if (t1 < 0) return false;
         x.t = t1;
         x.q0 = (int64_t)(t1 / p.H) * (2 * kBM);
@@ -125,6 +155,12 @@ struct FwdTiles {
         const bool two = x.q0 + kBM < p.T;
         x.hi[1] = two ? x.hi[0] + 1 : -1;
         x.lo[1] = two ? b1 / kBN : 0;
+        if constexpr (SINK) {
+            x.slo[0] = a0 / kBN;
+            x.shi[0] = min(sink_block(a0), x.lo[0] - 1);
+            x.slo[1] = two ? b0 / kBN : 0;
+            x.shi[1] = two ? min(sink_block(b0), x.lo[1] - 1) : -1;
+        }
         ++idx;
         t1 = t2;
         t2 = idx + 1 < end ? p.cta_tiles[idx + 1] : -1;
@@ -199,11 +235,12 @@ __device__ __noinline__ bool exchange_partial(uint8_t* smem, uint64_t* bars, uin
 // heads of 64), at the rate of one slot's chain for each, with 84 SMs idle.  Each rank takes
 // the other's maxima, sums and output of the slot of its own number through distributed shared memory and combines: 28.4 ->
 // 21.5 us there, one sample of 4096 tokens, 4 heads of 128: 55.3 -> 38.1.
-template <int D, bool PAIR>
+template <int D, bool PAIR, bool SINK>
 __global__ void __launch_bounds__(kFwdThreads, 1)
 k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
            const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_out, const FwdParams p) {
     using L = FwdSmem<D>;
+    static_assert(!(PAIR && SINK), "a shared tile is one run of blocks");
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBarOff);
@@ -284,8 +321,8 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
         if (elect_one()) {  // one elected thread runs the whole role
             uint32_t ring = 0, qcnt = 0;
             bool ok = true;
-            FwdTiles tiles(p, tile_begin, tile_end);
-            FwdTile x;
+            FwdTiles<SINK> tiles(p, tile_begin, tile_end);
+            FwdTile<SINK> x;
             while (ok && !(p.inject_stall && (!PAIR || cluster_rank() == 1)) && tiles.next(x)) {
                 if (PAIR && !x.take_half(cluster_rank())) continue;
                 const bool act1 = x.hi[1] >= 0;
@@ -293,7 +330,7 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
                 for (int hh = 0; hh < heads_per_shard && ok; ++hh) {
                     const int h = (x.t % p.H) * heads_per_shard + hh;
                     const int kvh = h / G;
-                    for (int j = top; j >= x.lo[0] && ok; --j) {
+                    for (int j = top; (SINK ? j >= 0 : j >= x.lo[0]) && ok; j = SINK ? x.after(j, 0) : j - 1) {
                         for (int kv = 0; kv < 2; ++kv) {  // K_j then V_j
                             const uint32_t st = ring % L::kStages;
                             ok = mbar_wait(&bar_empty[st], ((ring / L::kStages) & 1) ^ 1, abort_flag);
@@ -360,12 +397,12 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
                 }
                 if (kk1 == kBN / 16) tc_commit(&bar_odone[g]);
             };
-            FwdTiles tiles(p, tile_begin, tile_end);
-            FwdTile x;
+            FwdTiles<SINK> tiles(p, tile_begin, tile_end);
+            FwdTile<SINK> x;
             while (ok && tiles.next(x)) {
                 if (PAIR && !x.take_half(cluster_rank())) continue;
                 const bool act1 = x.hi[1] >= 0;
-                const int top = act1 ? x.hi[1] : x.hi[0], lo = x.lo[0];
+                const int top = act1 ? x.hi[1] : x.hi[0], last = x.last();
                 for (int hh = 0; hh < heads_per_shard && ok; ++hh) {
                     // prologue: S of the top block (slot 1's diagonal block; slot 0's when the tile has no slot 1)
                     uint32_t st = ring % L::kStages;
@@ -377,18 +414,20 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
                     issue_s(act1 ? 1 : 0, st);
                     if (PAIR && act1 && x.hi[0] == top) issue_s(0, st);   // the lower half of a shared tile
                     tc_commit(&bar_empty[st]);
-                    if (lo == top) tc_commit(bar_qempty);  // no later MMA of this tile reads Q
+                    if (last == top) tc_commit(bar_qempty);  // no later MMA of this tile reads Q
                     ++ring;
-                    for (int j = top; j >= lo && ok; --j) {
+                    int jn = 0;
+                    for (int j = top; j >= last && ok; j = jn) {
+                        jn = SINK && j != last ? x.after(j, 0) : j - 1;
                         const uint32_t st_v = ring % L::kStages;
                         const uint32_t ph_v = (ring / L::kStages) & 1;
                         ++ring;
-                        const bool more = j - 1 >= lo;
+                        const bool more = j != last;
                         const uint32_t st_k = ring % L::kStages;
                         bool have_k = false, have_v = false;
 #pragma unroll
                         for (int g = 0; g < 2; ++g) {
-                            if (j >= x.lo[g] && j <= x.hi[g]) {
+                            if (x.sees(g, j)) {
                                 if (!have_v) { ok = mbar_wait(&bar_full[st_v], ph_v, abort_flag); have_v = true; }
                                 if (ok) ok = mbar_wait(&bar_ppart[g], pcnt[g] & 1, abort_flag);   // P of the first kPFirst keys
                                 if (!ok) break;
@@ -400,7 +439,7 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
                                 tc_fence_after();
                                 issue_pv(g, st_v, j != x.hi[g], kPFirst / 16, kBN / 16);
                             }
-                            if (more && j - 1 >= x.lo[g] && j - 1 <= x.hi[g]) {
+                            if (more && x.sees(g, jn)) {
                                 if (!have_k) { ok = mbar_wait(&bar_full[st_k], (ring / L::kStages) & 1, abort_flag); have_k = true; }
                                 if (!ok) break;
                                 issue_s(g, st_k);
@@ -409,8 +448,8 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
                         if (!ok) break;
                         tc_commit(&bar_empty[st_v]);
                         if (more) { tc_commit(&bar_empty[st_k]); ++ring; }
-                        if (j - 1 == lo) tc_commit(bar_qempty);  // S(lo) was the last reader of Q: the next
-                    }                                            // tile's Q load overlaps the last block
+                        if (more && jn == last) tc_commit(bar_qempty);  // S(last) was the last reader of Q: the next
+                    }                                                   // tile's Q load overlaps the last block
                 }
             }
             if (!ok || abort_flag[0]) {   // give-up path: the MMAs already issued finish before TMEM is freed
@@ -447,8 +486,8 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
             tmem_st_wait();
             return true;
         };
-        FwdTiles tiles(p, tile_begin, tile_end);
-        FwdTile x;
+        FwdTiles<SINK> tiles(p, tile_begin, tile_end);
+        FwdTile<SINK> x;
         while (ok && tiles.next(x)) {
             if (PAIR && !x.take_half(cluster_rank())) continue;
             const int64_t qs = x.q0 + g * kBM;
@@ -461,13 +500,18 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
             const int64_t row = qs + row_in_tile;
             const bool row_ok = row < p.T;
             const int kstart = row_ok ? p.tok_start[row] : 0;
+            int sink_lo = 0, sink_hi = -1;   // SINK: the row's sinks ahead of its window
+            if (SINK && row_ok) {
+                sink_lo = p.tok_first[row];
+                sink_hi = (int)min((int64_t)sink_lo + p.sinks, (int64_t)kstart) - 1;
+            }
             // last valid row of the slot decides which blocks need the sample-start mask
             const int64_t last_row = (qs + kBM <= p.T ? qs + kBM : p.T) - 1;
             const int max_kstart = p.tok_start[last_row];
             for (int hh = 0; hh < heads_per_shard && ok; ++hh) {
                 const int h = (x.t % p.H) * heads_per_shard + hh;
                 float m_ref = -INFINITY, l_sum = 0.f;
-                for (int j = hi; j >= lo && ok; --j) {
+                for (int j = hi; (SINK ? j >= 0 : j >= lo) && ok; j = SINK ? x.after(j, g) : j - 1) {
                     ok = warp_wait(&bar_sfull[g], scnt & 1, abort_flag);
                     if (!ok) break;
                     ++scnt;
@@ -484,7 +528,8 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
                         const int c_hi = row_ok ? (int)(row - k0) : kBN;     // last visible column
 #pragma unroll
                         for (int w = 0; w < kBN / 32; ++w) {
-                            const uint32_t vis = range_bits(c_lo - 32 * w, c_hi - 32 * w);
+                            uint32_t vis = range_bits(c_lo - 32 * w, c_hi - 32 * w);
+                            if (SINK) vis |= range_bits(sink_lo - k0 - 32 * w, sink_hi - k0 - 32 * w);
 #pragma unroll
                             for (int i = 0; i < 32; ++i) sr[32 * w + i] = (vis >> i) & 1u ? sr[32 * w + i] : 0xff800000u;  // -inf
                         }
@@ -655,21 +700,21 @@ int make_f32_3d_map(CUtensorMap* m, const void* base, int64_t T, int H, int d, i
     return r == CUDA_SUCCESS ? LIBRA_OK : LIBRA_ERR_CUDA;
 }
 
-template <int D, bool PAIR>
+template <int D, bool PAIR, bool SINK = false>
 static int launch_fwd(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tout,
                       const FwdParams& prm, int W, libra_plan_t* mp, cudaStream_t s) {
     using L = FwdSmem<D>;
-    constexpr int kSlot = (D == 128 ? 0 : 1) + (PAIR ? 5 : 0);
+    constexpr int kSlot = (D == 128 ? 0 : 1) + (PAIR ? 5 : (SINK ? 12 : 0));
     if (!cfg_done(kSlot)) {   // per device: the attribute belongs to the device's copy of the kernel
-        if (cudaFuncSetAttribute(k_attn_fwd<D, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kAlloc) != cudaSuccess)
+        if (cudaFuncSetAttribute(k_attn_fwd<D, PAIR, SINK>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kAlloc) != cudaSuccess)
             return LIBRA_ERR_CUDA;
-        if (!regs_pool_ok(k_attn_fwd<D, PAIR>, 256, LIBRA_FWD_REG_INC, 128, LIBRA_FWD_REG_DEC)) return LIBRA_ERR_UNSUPPORTED;
+        if (!regs_pool_ok(k_attn_fwd<D, PAIR, SINK>, 256, LIBRA_FWD_REG_INC, 128, LIBRA_FWD_REG_DEC)) return LIBRA_ERR_UNSUPPORTED;
         cfg_mark(kSlot);
     }
     count_launch();
     mp->n_outcome[0] = PAIR ? W / 2 * 2 : W;
-    const cudaError_t e = launch_dependent<PAIR ? 2 : 1>(k_attn_fwd<D, PAIR>, mp->n_outcome[0], kFwdThreads, L::kAlloc, s, tq, tk, tv,
-                                                         tout, prm);
+    const cudaError_t e = launch_dependent<PAIR ? 2 : 1>(k_attn_fwd<D, PAIR, SINK>, mp->n_outcome[0], kFwdThreads, L::kAlloc, s,
+                                                         tq, tk, tv, tout, prm);
     return e == cudaSuccess ? LIBRA_OK : LIBRA_ERR_CUDA;
 }
 
@@ -715,6 +760,8 @@ extern "C" int libra_attn_pool_fwd(const void* q_dev, const void* k_dev, const v
     prm.cta_offsets = d.d_cta_offsets;
     prm.cta_tiles = d.d_cta_exec;
     prm.tok_start = plan->d_tok_start;
+    prm.tok_first = plan->d_tok_first;
+    prm.sinks = plan->sinks;
     prm.T = plan->T;
     prm.hq = dims->hq;
     prm.hkv = dims->hkv;
@@ -731,8 +778,13 @@ extern "C" int libra_attn_pool_fwd(const void* q_dev, const void* k_dev, const v
     // exchange goes through the spent ring) and samples, empty ones counted, average four key blocks (the longest, which
     // bounds the launch, is not known here): 4000 tokens, 4 heads of 128, in samples of up to 300 / 800 / 4000 tokens took
     // 12.0 / 18.0 / 55.3 us with one CTA a tile and 14.0 / 18.4 / 38.1 with two.
-    const bool pair = d.NT <= d.W / 2 && d.H == dims->hq && plan->T >= 4 * kBN * (int64_t)plan->n;
-    if (dims->head_dim == 128)
+    // (A window of fewer blocks leaves no tile of kShareBlocks; tiles with sinks are not shared.)
+    const bool pair = d.NT <= d.W / 2 && d.H == dims->hq && plan->T >= 4 * kBN * (int64_t)plan->n && plan->sinks == 0 &&
+                      (plan->window == 0 || plan->window > (kShareBlocks - 3) * kBN);
+    if (plan->sinks)
+        rc = dims->head_dim == 128 ? launch_fwd<128, false, true>(tq, tk, tv, tout, prm, d.W, mp, s)
+                                   : launch_fwd<64, false, true>(tq, tk, tv, tout, prm, d.W, mp, s);
+    else if (dims->head_dim == 128)
         rc = pair ? launch_fwd<128, true>(tq, tk, tv, tout, prm, d.W, mp, s) : launch_fwd<128, false>(tq, tk, tv, tout, prm, d.W, mp, s);
     else
         rc = pair ? launch_fwd<64, true>(tq, tk, tv, tout, prm, d.W, mp, s) : launch_fwd<64, false>(tq, tk, tv, tout, prm, d.W, mp, s);

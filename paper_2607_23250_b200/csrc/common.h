@@ -35,6 +35,9 @@ struct PlanDir {
     int32_t* d_u_chunk = nullptr;      // [NB] query chunk of pair-block u
     int32_t* d_first_j = nullptr;      // [chunks] first key block of a query chunk
     int64_t* d_base = nullptr;         // [chunks + 1] its pair-block
+    // plans with sinks: the key blocks ahead of first_j that rows of the chunk see all the same (pair-blocks base .. base + n - 1)
+    int32_t* d_sink_j = nullptr;       // [chunks] first of them
+    int32_t* d_sink_n = nullptr;       // [chunks] their number
 };
 
 }  // namespace libra
@@ -50,8 +53,13 @@ struct libra_plan {
     int n_blocks = 0;
     bool plain_memory = false;       // built while its stream was being captured: the blocks are not stream-ordered
     int other_stream = 0;            // built or used on a stream other than the legacy one
-    int32_t* d_tok_start = nullptr;  // [T] first token of the sample that holds token t
-    int32_t* d_tok_end = nullptr;    // [T] one past the last token of that sample
+    int window = 0;                  // positions a query sees, its own among them; 0: all of its sample's
+    int sinks = 0;                   // first positions of a sample that stay visible beyond the window
+    int32_t* d_tok_start = nullptr;  // [T] first key that query t sees, the sinks ahead of its window left out
+    int32_t* d_tok_end = nullptr;    // [T] one past the last query that sees key t
+    int32_t* d_tok_first = nullptr;  // [T] first token of the sample that holds token t; plans with sinks only
+    int32_t* d_blk_end = nullptr;    // [ceil(T / 128)] the largest tok_end among the block's keys
+    int32_t* d_blk_min = nullptr;    // [ceil(T / 128)] at most the smallest of them
     int* d_status = nullptr;         // the planner's verdict on cu_seqlens
     // Outcome of each CTA of the last launch of a kernel (0 or LIBRA_ERR_*), written by every CTA when it leaves, so
     // that nothing has to be cleared before a launch: forward; dK/dV, fused or dV pass; dK pass; dQ kernel or pass.
@@ -78,7 +86,7 @@ namespace libra {
 // attributes are per device, so the flag is kept per device ordinal; `slot` is a small integer the
 // caller picks per kernel family.  Returns true when this (device, slot) has been configured.
 constexpr int kMaxDevices = 64;
-constexpr int kCfgSlots = 16;
+constexpr int kCfgSlots = 24;
 bool cfg_done(int slot);
 void cfg_mark(int slot);
 // LIBRA_ERR_PLAN_MISMATCH when the current device is not the one the plan was built on.

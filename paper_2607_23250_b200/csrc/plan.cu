@@ -75,12 +75,17 @@ cudaError_t scratch_alloc(void** p, size_t bytes, cudaStream_t s) {
 
 // ---- kernels --------------------------------------------------------------------------------
 
-// cu_seqlens checks (starts at 0, non-decreasing, ends at T) and, for every token, the bounds [start, end) of the sample
-// that holds it.  The search keeps every index inside [0, n] whatever cu contains, and the bounds are clamped to
+// cu_seqlens checks (starts at 0, non-decreasing, ends at T) and, for every token, the first key it sees as a query and the end
+// of the queries that see it as a key: the bounds [a, e) of its sample, cut by the window; a sink is seen up to the end of its
+// sample.  Of each block of 128 keys the largest of the ends: that of the last key, unless a sink of its sample lies in
+// the block (every other sample of the block ends in it); and a bound from below.  The search keeps every index inside [0, n] whatever cu contains, and the bounds are clamped to
 // start <= t < end <= T, so that a malformed cu_seqlens (flagged in *status) can never make a
 // later kernel form an address outside its tensors.
-__global__ void k_token_bounds(const int32_t* __restrict__ cu, int n, int64_t T, int32_t* __restrict__ tok_start,
-                               int32_t* __restrict__ tok_end, int* status) {
+struct TokenBounds {
+    int32_t *tok_start, *tok_end, *tok_first, *blk_end, *blk_min;   // tok_first: null without sinks
+    int64_t window, sinks;                                          // window: T where there is none
+};
+__global__ void k_token_bounds(const int32_t* __restrict__ cu, int n, int64_t T, const TokenBounds out, int* status) {
     const int64_t t = blockIdx.x * (int64_t)blockDim.x + threadIdx.x;
     if (t <= n) {
         bool bad = false;
@@ -95,10 +100,43 @@ __global__ void k_token_bounds(const int32_t* __restrict__ cu, int n, int64_t T,
         const int mid = (lo + hi) >> 1;
         if (cu[mid] <= t) lo = mid; else hi = mid;
     }
-    const int64_t a = cu[lo], e = cu[lo + 1];
-    tok_start[t] = (int32_t)(a < 0 ? 0 : (a > t ? t : a));
-    tok_end[t] = (int32_t)(e < t + 1 ? t + 1 : (e > T ? T : e));
+    int64_t a = cu[lo], e = cu[lo + 1];
+    a = a < 0 ? 0 : (a > t ? t : a);
+    e = e < t + 1 ? t + 1 : (e > T ? T : e);
+    const int64_t near = t + out.window < e ? t + out.window : e;   // one past the last query whose window holds t
+    out.tok_start[t] = (int32_t)(t - out.window + 1 > a ? t - out.window + 1 : a);
+    out.tok_end[t] = (int32_t)(t - a < out.sinks ? e : near);
+    if (out.tok_first) out.tok_first[t] = (int32_t)a;
+    if (t % 128 == 0) out.blk_min[t / 128] = (int32_t)near;
+    if (t % 128 == 127 || t == T - 1) out.blk_end[t / 128] = (int32_t)(a + out.sinks > t / 128 * 128 ? e : near);
 }
+
+// The mask as the planning kernels see it.
+struct MaskView {
+    const int32_t *tok_start, *tok_end, *tok_first;   // tok_first: null without sinks
+    int64_t T, window, sinks;                         // window: T where there is none
+    // Keys [k0, last] are seen by queries up to this one (exclusive): see k_token_bounds.  A sink of the last key's sample,
+    // where the range holds one, is the first key of the range or of the sample.
+    __device__ __forceinline__ int64_t key_end(int64_t k0, int64_t last) const {
+        if (tok_first) {
+            const int64_t a = tok_first[last];
+            if (a + sinks > k0) return tok_end[a > k0 ? a : k0];
+        }
+        return tok_end[last];
+    }
+    // The same without the sinks' reach beyond the window: never decreases with `last`.
+    __device__ __forceinline__ int64_t near_end(int64_t last) const {
+        const int64_t e = tok_end[last];
+        return e < last + window ? e : last + window;
+    }
+    // Sinks of query t's sample ahead of its window: [first, end), empty when end <= first.
+    __device__ __forceinline__ int64_t early_end(int64_t t, int64_t& first) const {
+        first = tok_first ? tok_first[t] : 0;
+        if (!tok_first) return 0;
+        const int64_t start = tok_start[t];
+        return first + sinks < start ? first + sinks : start;
+    }
+};
 
 // What the kernels below need of one direction; the directions of a plan share launches.
 struct DirView {
@@ -119,15 +157,18 @@ struct DirViews {
 
 // Weight of block b (Eq. 6): a token at position p of a sample of length len contributes
 // p + 1 pairs as a query (keys 0..p) and len - p pairs as a key (queries p..len-1).
+// With a window and sinks the same counts of visible pairs.
 // Block-count weight (LIBRA_WEIGHT_BLOCKS): the token axis is cut into chunks at multiples of g.  For a
 // chunk of query rows [r0, r1] the visible keys span the chunks from the one holding the first key of r0's
 // sample to the one holding r1 (row r0 sees a key in every chunk of that range, later rows see no chunk
 // outside it); for a chunk of keys [c0, c1] the attending queries span the chunks from the one holding c0
-// to the one holding the last token of c1's sample.
+// to the one holding the last token of c1's sample.  (With sinks r0 also sees a run of chunks ahead of its window, and
+// the last query of a chunk that holds a sink is that of the sink's sample.)
 // One warp per block (a thread per block read its tokens one after the other: 20 us at 32768 tokens, 4 now).
-__global__ void k_block_weights(const int32_t* __restrict__ tok_start, const int32_t* __restrict__ tok_end,
-                                int64_t T, const DirViews views) {
+__global__ void k_block_weights(const MaskView m, const DirViews views) {
     const DirView& d = views.v[blockIdx.y];
+    const int32_t *tok_start = m.tok_start, *tok_end = m.tok_end;
+    const int64_t T = m.T;
     const int64_t b = (blockIdx.x * (int64_t)blockDim.x + threadIdx.x) >> 5;
     const int lane = threadIdx.x & 31;
     if (b >= d.NB) return;
@@ -136,13 +177,30 @@ __global__ void k_block_weights(const int32_t* __restrict__ tok_start, const int
     int64_t w = 0;
     if (d.g == 0) {
         for (int64_t t = t0 + lane; t < t1; t += 32)
-            w += d.key_major ? (int64_t)tok_end[t] - t : t - (int64_t)tok_start[t] + 1;
+            if (d.key_major) {
+                w += (int64_t)tok_end[t] - t;
+            } else {
+                int64_t a;
+                const int64_t e = m.early_end(t, a);
+                w += t - (int64_t)tok_start[t] + 1 + (e > a ? e - a : 0);
+            }
     } else {
         for (int64_t c = t0 / d.g + lane; c * d.g < t1; c += 32) {
             const int64_t first = c * d.g > t0 ? c * d.g : t0;
             const int64_t last = ((c + 1) * d.g < t1 ? (c + 1) * d.g : t1) - 1;
-            const int64_t n = d.key_major ? ((int64_t)tok_end[last] - 1) / d.g - first / d.g + 1
-                                          : last / d.g - (int64_t)tok_start[first] / d.g + 1;
+            int64_t n;
+            if (d.key_major) {
+                n = (m.key_end(first, last) - 1) / d.g - first / d.g + 1;
+            } else {
+                const int64_t lo = (int64_t)tok_start[first] / d.g;
+                int64_t a;
+                const int64_t e = m.early_end(first, a);
+                n = last / d.g - lo + 1;
+                if (e > a) {
+                    const int64_t top = (e - 1) / d.g < lo - 1 ? (e - 1) / d.g : lo - 1;   // (a chunk of the window counts once)
+                    if (top >= a / d.g) n += top - a / d.g + 1;
+                }
+            }
             w += 8 * n + d.unit_cost;
         }
     }
@@ -308,24 +366,38 @@ __global__ void k_check_loads(const DirView d, int* __restrict__ status) {
 // ---- pair tiles: key block x query chunk x head (the fused backward's units) ---------------------------------
 // The score matrix in tile x tile cells: cell (i, j) is live when a query of row block i attends a key of key
 // block j; for a key block the live cells are the row blocks j .. last(j), last(j) = the block of the last token
-// of the sample that holds the key block's last key.  Pair-block (c, j) = key block j against the R = chunk / tile
+// of the sample that holds the key block's last key (with a window or sinks: of the last query that sees one of its
+// keys).  Pair-block (c, j) = key block j against the R = chunk / tile
 // row blocks of query chunk c, present when one of them is live; numbered chunk by chunk, key blocks ascending.
-// last(j) never decreases with j, so the key blocks of a chunk are the range first(c) .. min(NKB, (c+1) R) - 1.
+// last(j) never decreases with j, so the key blocks of a chunk are the range first(c) .. min(NKB, (c+1) R) - 1.  Sinks are
+// the exception: the blocks that hold sinks of the sample which the chunk's first row belongs to are seen by that row, wherever
+// they lie; those below first(c), a range too, come first.
 // Key blocks of kt tokens against row blocks of rt tokens (kt a multiple of rt; the pair tiles proper have kt = rt).
-__device__ __forceinline__ int64_t pair_last_row_block(const int32_t* tok_end, int64_t T, int kt, int rt, int64_t j) {
-    const int64_t last_key = ((j + 1) * kt < T ? (j + 1) * kt : T) - 1;
-    return ((int64_t)tok_end[last_key] - 1) / rt;
+__device__ __forceinline__ int64_t pair_last_row_block(const MaskView& m, int kt, int rt, int64_t j) {
+    const int64_t last_key = ((j + 1) * kt < m.T ? (j + 1) * kt : m.T) - 1;
+    return (m.key_end(j * kt, last_key) - 1) / rt;
+}
+// Without the sinks' reach.
+__device__ __forceinline__ int64_t pair_near_row_block(const MaskView& m, int kt, int rt, int64_t j) {
+    const int64_t last_key = ((j + 1) * kt < m.T ? (j + 1) * kt : m.T) - 1;
+    return (m.near_end(last_key) - 1) / rt;
 }
 // Chunk sizes under consideration, for the tiles proper and the wide ones: one block each finds the key-block range of
 // every query chunk, the exclusive prefix sum of the counts and their total (base[NC] and totals[block]); one more block
 // for either finds the most live cells of a key block (totals[kPairCands + k]) and the sum over all of them
 // (totals[kPairCands + 2 + k]).
-struct PairTables { int dir = 0, kt = 0, R = 0; int32_t* first_j = nullptr; int32_t* count = nullptr; int64_t* base = nullptr; int64_t NC = 0; };
+struct PairTables {
+    int dir = 0, kt = 0, R = 0;
+    int32_t *first_j = nullptr, *count = nullptr, *sink_j = nullptr, *sink_n = nullptr;   // (the last two: plans with sinks)
+    int64_t* base = nullptr;
+    int64_t NC = 0;
+};
 constexpr int kChunkSizes = 6, kPairCands = 3 * kChunkSizes, kPairTotals = kPairCands + 4;
 struct PairCands { PairTables c[kPairCands]; int n = 0; int rt = 0; int kt[2] = {}; int n_longest = 0; };
-__global__ void __launch_bounds__(1024) k_pair_chunks(const int32_t* __restrict__ tok_end, int64_t T, const __grid_constant__ PairCands cands,
+__global__ void __launch_bounds__(1024) k_pair_chunks(const __grid_constant__ MaskView m, const __grid_constant__ PairCands cands,
                                                       int64_t* __restrict__ totals) {
     const int rt = cands.rt;
+    const int64_t T = m.T;
     if ((int)blockIdx.x >= cands.n) {
         __shared__ int longest;
         __shared__ unsigned long long cells;
@@ -335,7 +407,7 @@ __global__ void __launch_bounds__(1024) k_pair_chunks(const int32_t* __restrict_
         int most = 0;
         unsigned long long sum = 0;
         for (int64_t j = threadIdx.x; j * kt < T; j += 1024) {
-            const int64_t n = pair_last_row_block(tok_end, T, kt, rt, j) - j * kt / rt + 1;
+            const int64_t n = pair_last_row_block(m, kt, rt, j) - j * kt / rt + 1;
             most = n > most ? (int)n : most;
             sum += n;
         }
@@ -362,11 +434,19 @@ __global__ void __launch_bounds__(1024) k_pair_chunks(const int32_t* __restrict_
             int64_t lo = 0, hi = NKB;   // first j with last(j) / R >= c
             while (lo < hi) {
                 const int64_t mid = (lo + hi) >> 1;
-                if (pair_last_row_block(tok_end, T, kt, rt, mid) / R >= c) hi = mid; else lo = mid + 1;
+                if (pair_near_row_block(m, kt, rt, mid) / R >= c) hi = mid; else lo = mid + 1;
             }
             const int64_t end = ((c + 1) * R * rt - 1) / kt;   // the key block of the chunk's last row
             const int64_t last = end < NKB - 1 ? end : NKB - 1;
             n = last >= lo ? last - lo + 1 : 0;
+            if (m.tok_first) {
+                const int64_t a = m.tok_first[c * R * rt], e = a + m.sinks < c * R * rt ? a + m.sinks : c * R * rt;
+                const int64_t j0 = a / kt, top = (e - 1) / kt < lo - 1 ? (e - 1) / kt : lo - 1;
+                const int64_t early = e > a && top >= j0 ? top - j0 + 1 : 0;
+                t.sink_j[c] = (int32_t)j0;
+                t.sink_n[c] = (int32_t)early;
+                n += early;
+            }
             first_j[c] = (int32_t)lo;
             count[c] = (int32_t)n;
         }
@@ -384,15 +464,14 @@ __global__ void __launch_bounds__(1024) k_pair_chunks(const int32_t* __restrict_
     if (threadIdx.x == 0) { base[NC] = run; totals[blockIdx.x] = run; }
 }
 // Weight of pair-block (c, j): its live cells, min(last(j), c R + R - 1) - max(j, c R) + 1.
-__global__ void k_pair_fill(const int32_t* __restrict__ tok_end, int64_t T, int kt, int rt, int R, int64_t NC,
-                            const int32_t* __restrict__ first_j, const int32_t* __restrict__ count,
-                            const int64_t* __restrict__ base, int32_t* __restrict__ u_blk,
-                            int32_t* __restrict__ u_chunk, int64_t* __restrict__ weight_blk) {
+__global__ void k_pair_fill(const __grid_constant__ MaskView m, int rt, const __grid_constant__ PairTables t,
+                            int32_t* __restrict__ u_blk, int32_t* __restrict__ u_chunk, int64_t* __restrict__ weight_blk) {
     const int64_t c = blockIdx.x;
-    if (c >= NC) return;
-    for (int x = threadIdx.x; x < count[c]; x += blockDim.x) {
-        const int64_t j = first_j[c] + x, u = base[c] + x;
-        const int64_t last = pair_last_row_block(tok_end, T, kt, rt, j), first = j * kt / rt;
+    if (c >= t.NC) return;
+    const int R = t.R, kt = t.kt, early = m.tok_first ? t.sink_n[c] : 0;
+    for (int x = threadIdx.x; x < t.count[c]; x += blockDim.x) {
+        const int64_t j = x < early ? t.sink_j[c] + x : t.first_j[c] + x - early, u = t.base[c] + x;
+        const int64_t last = pair_last_row_block(m, kt, rt, j), first = j * kt / rt;
         const int64_t i0 = first > c * R ? first : c * R, i1 = last < c * R + R - 1 ? last : c * R + R - 1;
         u_blk[u] = (int32_t)j;
         u_chunk[u] = (int32_t)c;
@@ -543,12 +622,12 @@ static bool fused_on_pairs(const libra_plan* p, int64_t cells, int64_t wide_cell
 static double heads_per_kv(const libra_plan* p) { return p->dir[0].H > p->dir[2].H ? (double)p->dir[0].H / p->dir[2].H : 1.0; }
 // Counts, choice and, while every size has more than 262144 pair-blocks, twice the largest.  `pairs`: whether the fused kernel's
 // wide tiles are under consideration, and whether they were taken.
-static int count_pair_blocks(libra_plan* p, PairCands& cands, int64_t* d_totals, PairTables (&chosen)[libra_plan::kDirs], double G,
+static int count_pair_blocks(libra_plan* p, const MaskView& mask, PairCands& cands, int64_t* d_totals, PairTables (&chosen)[libra_plan::kDirs], double G,
                              bool own_choice, bool& pairs) {
     const int dirs = cands.n_longest;
     for (;;) {
         int64_t totals[kPairTotals];
-        k_pair_chunks<<<cands.n + dirs, 1024, 0, p->stream>>>(p->d_tok_end, p->T, cands, d_totals);
+        k_pair_chunks<<<cands.n + dirs, 1024, 0, p->stream>>>(mask, cands, d_totals);
         count_launch();
         if (cudaMemcpyAsync(totals, d_totals, sizeof(totals), cudaMemcpyDeviceToHost, p->stream) != cudaSuccess ||
             cudaStreamSynchronize(p->stream) != cudaSuccess)
@@ -626,6 +705,9 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
         zero_bytes = c.used;
         c.take(&p->d_tok_start, T);
         c.take(&p->d_tok_end, T);
+        if (p->sinks) c.take(&p->d_tok_first, T);
+        c.take(&p->d_blk_end, (T + 127) / 128);
+        c.take(&p->d_blk_min, (T + 127) / 128);
         for (int k = 0; k < kDirs; ++k)
             if (sorted[k]) carve_dir(p->dir[k], c, false, false);
         if (want[2]) {
@@ -634,6 +716,7 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
                 PairTables& t = cands.c[x];
                 c.take(&t.first_j, t.NC);
                 c.take(&t.count, t.NC);
+                if (p->sinks) { c.take(&t.sink_j, t.NC); c.take(&t.sink_n, t.NC); }
                 c.take(&t.base, t.NC + 1);
             }
         }
@@ -644,11 +727,14 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
     carve(mem);
     cudaMemsetAsync(mem.at, 0, zero_bytes, s);
     const int64_t span = T > p->n + 1 ? T : p->n + 1;
-    k_token_bounds<<<grid_for(span, 256), 256, 0, s>>>(cu, p->n, T, p->d_tok_start, p->d_tok_end, p->d_status);
+    const int64_t window = p->window ? p->window : T;
+    const TokenBounds bounds = {p->d_tok_start, p->d_tok_end, p->d_tok_first, p->d_blk_end, p->d_blk_min, window, p->sinks};
+    const MaskView mask = {p->d_tok_start, p->d_tok_end, p->d_tok_first, T, window, p->sinks};
+    k_token_bounds<<<grid_for(span, 256), 256, 0, s>>>(cu, p->n, T, bounds, p->d_status);
     count_launch();
     // ---- pair tiles: their number comes back, then their arrays
     if (want[2]) {
-        if (const int rc = count_pair_blocks(p, cands, d_totals, chosen, heads_per_kv(p), o.pair_chunk == 0, pairs[4]); rc != LIBRA_OK)
+        if (const int rc = count_pair_blocks(p, mask, cands, d_totals, chosen, heads_per_kv(p), o.pair_chunk == 0, pairs[4]); rc != LIBRA_OK)
             return rc;
         Carver ps, pm;
         size_t pair_zero = 0;
@@ -657,6 +743,8 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
             if (const int rc = check_dir(p, p->dir[k], true); rc != LIBRA_OK) return rc;
             p->dir[k].d_first_j = chosen[k].first_j;
             p->dir[k].d_base = chosen[k].base;
+            p->dir[k].d_sink_j = chosen[k].sink_j;
+            p->dir[k].d_sink_n = chosen[k].sink_n;
         }
         auto carve_pairs = [&](Carver& c) {
             for (int k = 2; k < kDirs; ++k)
@@ -673,8 +761,7 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
             if (!pairs[k]) continue;
             PlanDir& d = p->dir[k];
             const PairTables& t = chosen[k];
-            k_pair_fill<<<(unsigned)t.NC, 128, 0, s>>>(p->d_tok_end, T, t.kt, cands.rt, t.R, t.NC, t.first_j, t.count, t.base, d.d_u_blk,
-                                                       d.d_u_chunk, d.d_weight_blk);
+            k_pair_fill<<<(unsigned)t.NC, 128, 0, s>>>(mask, cands.rt, t, d.d_u_blk, d.d_u_chunk, d.d_weight_blk);
             count_launch();
         }
     }
@@ -688,7 +775,7 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
             max_nb = p->dir[k].NB > max_nb ? p->dir[k].NB : max_nb;
         }
     if (n > 0) {
-        k_block_weights<<<dim3(grid_for(max_nb * 32, 256), n), 256, 0, s>>>(p->d_tok_start, p->d_tok_end, T, views);
+        k_block_weights<<<dim3(grid_for(max_nb * 32, 256), n), 256, 0, s>>>(mask, views);
         k_rank_blocks<<<dim3(grid_for(max_nb, 16), n), 256, 0, s>>>(views);
         count_launch(2);
     }
@@ -725,8 +812,9 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
 
 using namespace libra;
 
-extern "C" int libra_plan_tiles(const int32_t* cu_seqlens_dev, int n_samples, int n_heads, int tile_q,
-                                const libra_plan_opts* opts, void* stream, libra_plan_t** plan_out) {
+// window = 0: none.
+static int make_plan(const int32_t* cu_seqlens_dev, int n_samples, int n_heads, int tile_q, const libra_plan_opts* opts, int window,
+                     int sinks, void* stream, libra_plan_t** plan_out) {
     if (!cu_seqlens_dev || !plan_out || n_samples <= 0 || n_heads <= 0 || tile_q <= 0) return LIBRA_ERR_INVALID_ARG;
     *plan_out = nullptr;
     libra_plan_opts o = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
@@ -756,6 +844,8 @@ extern "C" int libra_plan_tiles(const int32_t* cu_seqlens_dev, int n_samples, in
     if (!p) return LIBRA_ERR_CUDA;
     p->T = T; p->n = n_samples; p->device = dev; p->sm_count = sms; p->stream = s;
     if (s) p->other_stream = 1;
+    p->window = window < T ? window : 0;                 // (every query sees all of its sample then, the sinks too)
+    p->sinks = p->window ? (sinks < T ? sinks : (int)T) : 0;
     p->W = o.n_workers ? o.n_workers : sms;
     const int dirs = o.directions ? o.directions : (LIBRA_DIR_Q | LIBRA_DIR_KV);
     const int tile_kv = o.tile_kv ? o.tile_kv : 128;
@@ -787,6 +877,18 @@ extern "C" int libra_plan_tiles(const int32_t* cu_seqlens_dev, int n_samples, in
     }
     *plan_out = p;
     return LIBRA_OK;
+}
+
+extern "C" int libra_plan_tiles(const int32_t* cu_seqlens_dev, int n_samples, int n_heads, int tile_q,
+                                const libra_plan_opts* opts, void* stream, libra_plan_t** plan_out) {
+    return make_plan(cu_seqlens_dev, n_samples, n_heads, tile_q, opts, 0, 0, stream, plan_out);
+}
+
+extern "C" int libra_plan_tiles_window(const int32_t* cu_seqlens_dev, int n_samples, int n_heads, int tile_q,
+                                       const libra_plan_opts* opts, int window, int sinks, void* stream,
+                                       libra_plan_t** plan_out) {
+    if (window < 1 || sinks < 0) return LIBRA_ERR_INVALID_ARG;
+    return make_plan(cu_seqlens_dev, n_samples, n_heads, tile_q, opts, window, sinks, stream, plan_out);
 }
 
 static PlanDir* dir_of(const libra_plan_t* plan, int direction) {

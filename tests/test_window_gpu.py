@@ -1,0 +1,243 @@
+"""Pool attention with a sliding window and sinks: planner, forward and both backward forms against the definition in 64 bits,
+with the bounds of window_reference.py."""
+import numpy as np
+import pytest
+import torch
+
+import window_reference as ref
+from paper_2607_23250_b200 import pools
+
+pytestmark = pytest.mark.gpu
+
+EDGES = [31, 32, 33, 32, 33, 64, 31, 96, 127, 33, 1, 32, 97, 126, 255, 2, 130]   # starts around words, blocks and tiles
+
+
+def _tensors(cu, hq, hkv, d, seed):
+    t = pools.make_tensors(int(cu[-1]), hq, hkv, d, seed=seed)
+    return [t[n].cuda() for n in ("q", "k", "v", "dout")]
+
+
+def _plan(cu, hq, hkv, fused, window, sinks, **kw):
+    from paper_2607_23250_b200 import binding as lb
+    directions = lb.LIBRA_DIR_Q | (lb.LIBRA_DIR_PAIR if fused else lb.LIBRA_DIR_KV)
+    plan = lb.libra_plan_tiles(torch.from_numpy(cu).cuda(), hq, 256, directions=directions, tile_kv=128, n_heads_kv=hkv,
+                               window=window, sinks=sinks, **kw)
+    assert plan.status() == 0
+    return plan
+
+
+def _run(plan, q, k, v, dout, fused):
+    from paper_2607_23250_b200 import binding as lb
+    out, lse = lb.libra_attn_pool_fwd(q, k, v, plan)
+    grads = lb.libra_attn_pool_bwd(q, k, v, out, lse, dout, plan)
+    torch.cuda.synchronize()
+    plan.busy_times(lb.KERNEL_FWD)                                   # raises when a bounded wait gave up
+    plan.busy_times(lb.KERNEL_BWD_FUSED if fused and q.shape[2] == 128 else lb.KERNEL_BWD_DQ)
+    return out, lse, grads
+
+
+def _check(cu, q, k, v, dout, got, window, sinks):
+    out, lse, grads = got
+    see = ref.visible(cu, window, sinks, "cuda")
+    o, l, b_o, b_l = ref.forward(q, k, v, see)
+    assert ref.worst(out, o, b_o) <= 1
+    assert ref.worst(lse, l, b_l) <= 1
+    want, bounds = ref.backward(q, k, v, out, lse, dout, see)
+    for name, g, w, b in zip(("dq", "dk", "dv"), grads, want, bounds):
+        assert ref.worst(g, w, b) <= 1, name
+
+
+def _case(lengths, hq, hkv, d, fused, window, sinks, seed=0, **kw):
+    cu = pools.cu_seqlens(lengths)
+    q, k, v, dout = _tensors(cu, hq, hkv, d, seed)
+    plan = _plan(cu, hq, hkv, fused, window, sinks, **kw)
+    got = _run(plan, q, k, v, dout, fused)
+    _check(cu, q, k, v, dout, got, window, sinks)
+    plan.destroy()
+
+
+FORMS = [(64, False), (128, False), (128, True), (256, False), (256, True)]
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (2, 3), (33, 0), (64, 5), (127, 128), (128, 1), (129, 40), (200, 0)])
+@pytest.mark.parametrize("d,fused", FORMS)
+def test_sample_bounds_at_word_and_block_edges(d, fused, window, sinks):
+    _case(EDGES, 2, 1, d, fused, window, sinks, seed=window)
+
+
+@pytest.mark.parametrize("lengths,window,sinks", [
+    ([1], 1, 0), ([1], 5, 5), ([2, 1], 1, 1), ([257], 3, 300), ([1500], 100, 4), ([1500], 500, 0), ([1500], 300, 260),
+    ([700, 40, 900], 129, 129), ([100, 1400], 384, 130), ([1000, 600], 640, 1), ([1600], 1599, 0), ([1600], 1, 1599),
+    ([130, 1, 1, 1400, 3], 257, 7)])
+@pytest.mark.parametrize("d,fused", FORMS)
+def test_long_and_mixed_samples(d, fused, lengths, window, sinks):
+    _case(lengths, 4, 2, d, fused, window, sinks, seed=sum(lengths))
+
+
+@pytest.mark.parametrize("seed", range(8))
+@pytest.mark.parametrize("d,fused", FORMS)
+def test_random_pools(d, fused, seed):
+    rng = np.random.default_rng([seed, d, fused])
+    lengths = pools.random_layout(rng, int(rng.integers(300, 2200)), int(rng.choice([5, 100, 700, 2200])))
+    hkv = int(rng.choice([1, 2]))
+    hq = hkv * int(rng.choice([1, 2, 3]))
+    window = int(np.exp(rng.uniform(0, np.log(1500))))
+    sinks = int(rng.choice([0, 1, 4, 128, 300]))
+    kw = dict(n_workers=int(rng.choice([0, 5, 36])))
+    if fused:
+        kw["pair_chunk"] = int(rng.choice([0, 128, 512]))
+    _case(lengths, hq, hkv, d, fused, window, sinks, seed=seed, **kw)
+
+
+@pytest.mark.parametrize("window,sinks", [(3000, 0), (3500, 4), (4000, 200), (3300, 130)])
+def test_fused_backward_on_pairs_of_ctas(window, sinks):
+    """Query chunks of 512 rows: sinks come as key blocks of their own, apart from the window's, in the later chunks; 130 and
+    200 sinks end in the second block of their first pair of key blocks, or fill both."""
+    lengths = [100, 7400]
+    cu = pools.cu_seqlens(lengths)
+    q, k, v, dout = _tensors(cu, 2, 1, 128, 3)
+    plan = _plan(cu, 2, 1, True, window, sinks, pair_chunk=512, n_workers=16)
+    assert plan.fused_ctas() == 2
+    got = _run(plan, q, k, v, dout, True)
+    _check(cu, q, k, v, dout, got, window, sinks)
+    from paper_2607_23250_b200 import binding as lb
+    assert bool((plan.tile_times(lb.KERNEL_BWD_FUSED) > 0).all())      # every pair tile was taken once
+    plan.destroy()
+
+
+@pytest.mark.parametrize("d,fused", FORMS)
+def test_a_window_that_reaches_everything_changes_nothing(d, fused):
+    from paper_2607_23250_b200 import binding as lb
+    cu = pools.cu_seqlens([300, 1, 800, 77])
+    q, k, v, dout = _tensors(cu, 4, 2, d, 9)
+    full = _plan(cu, 4, 2, fused, 0, 0)
+    wide = _plan(cu, 4, 2, fused, 800, 0)
+    a, b = (_run(p, q, k, v, dout, fused) for p in (full, wide))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    if not fused:
+        assert all(torch.equal(x, y) for x, y in zip(a[2], b[2]))
+    for direction in ((lb.LIBRA_DIR_Q, lb.LIBRA_DIR_PAIR) if fused else (lb.LIBRA_DIR_Q, lb.LIBRA_DIR_KV)):
+        x, y = full.export(direction), wide.export(direction)
+        assert all(np.array_equal(x[key], y[key]) for key in x)
+    full.destroy()
+    wide.destroy()
+
+
+@pytest.mark.parametrize("seed", range(10))
+def test_plan_weights_placement_and_pair_tiles(seed):
+    from paper_2607_23250_b200 import binding as lb
+    rng = np.random.default_rng(70 + seed)
+    lengths = pools.random_layout(rng, int(rng.integers(50, 2500)), int(rng.choice([7, 300, 2500])))
+    cu = pools.cu_seqlens(lengths)
+    window, sinks = int(rng.integers(1, 600)), int(rng.choice([0, 1, 5, 100, 400]))
+    see = ref.visible(cu, window, sinks)
+    H, Hkv, W = int(rng.integers(1, 4)), int(rng.integers(1, 3)), int(rng.integers(1, 50))
+    tile, tile_kv, g = int(rng.choice([16, 100, 256])), int(rng.choice([32, 64, 128])), int(rng.choice([0, 16, 128]))
+    chunk = tile_kv * int(rng.choice([1, 3, 8]))
+    kw = dict(weight_model=lb.LIBRA_WEIGHT_BLOCKS, cost_block=g, unit_cost_q=5, unit_cost_kv=3) if g else {}
+    plan = lb.libra_plan_tiles(torch.from_numpy(cu).cuda(), H, tile, n_workers=W, directions=7, tile_kv=tile_kv,
+                               n_heads_kv=Hkv, window=window, sinks=sinks, pair_chunk=chunk, **kw)
+    assert plan.status() == 0
+    for direction, heads, size, unit in ((lb.LIBRA_DIR_Q, H, tile, 5), (lb.LIBRA_DIR_KV, Hkv, tile_kv, 3)):
+        got = plan.export(direction)
+        want = ref.tile_weights(see, size, direction == lb.LIBRA_DIR_KV, g, unit)
+        assert got["weight"].tolist() == [w for w in want for _ in range(heads)]
+        cta, loads = ref.place(want, heads, W)
+        assert np.array_equal(got["cta_of_tile"], cta) and np.array_equal(got["loads"], loads)
+    if not g:
+        q_w, kv_w = (plan.export(x)["weight"].sum() for x in (lb.LIBRA_DIR_Q, lb.LIBRA_DIR_KV))
+        assert q_w == H * int(see.sum()) and kv_w == Hkv * int(see.sum())
+    want = ref.live_pairs(see, tile_kv, chunk)
+    kb, qc, size = plan.export_pairs()
+    assert size == chunk
+    assert list(zip(qc.tolist(), kb.tolist())) == [(c, j) for c, j, _ in want]
+    assert plan.export(lb.LIBRA_DIR_PAIR)["weight"].tolist() == [n for _ in range(Hkv) for *_, n in want]
+    plan.destroy()
+
+
+def test_refusals():
+    from paper_2607_23250_b200 import binding as lb
+    cu = torch.tensor([0, 300], dtype=torch.int32).cuda()
+    for window, sinks in ((-1, 0), (0, 3), (5, -1)):
+        with pytest.raises(lb.LibraError) as err:
+            lb.libra_plan_tiles(cu, 1, 256, window=window, sinks=sinks)
+        assert err.value.code == lb.ERR_INVALID_ARG
+    bad = torch.tensor([0, 200, 100, 300], dtype=torch.int32).cuda()
+    plan = lb.libra_plan_tiles(bad, 1, 256, directions=7, tile_kv=128, total_tokens=300, window=20, sinks=3)
+    assert plan.status() == lb.ERR_BAD_SEQLENS
+    t = pools.make_tensors(300, 1, 1, 128, seed=1, device="cuda")
+    out = torch.full_like(t["q"], 7.0)
+    lb.libra_attn_pool_fwd(t["q"], t["k"], t["v"], plan, out=out)
+    assert bool((out == 7).all())
+    plan.destroy()
+
+
+def test_two_kernel_form_is_bit_reproducible_and_captured():
+    """Twice the same bits, eagerly and replayed from a graph with other inputs in between; on a stream of its own."""
+    from paper_2607_23250_b200 import binding as lb
+    cu = pools.cu_seqlens([900, 20, 1100])
+    q, k, v, dout = _tensors(cu, 4, 2, 128, 5)
+    plan = _plan(cu, 4, 2, False, 250, 6)
+    a = _run(plan, q, k, v, dout, False)
+    b = _run(plan, q, k, v, dout, False)
+    same = lambda x, y: torch.equal(x[0], y[0]) and torch.equal(x[1], y[1]) and all(torch.equal(g, h) for g, h in zip(x[2], y[2]))  # noqa: E731
+    assert same(a, b)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        out, lse = torch.empty_like(q), torch.empty((4, q.shape[0]), device="cuda")
+        grads = [torch.empty_like(x) for x in (q, k, v)]
+        ws = torch.empty(lb.libra_attn_pool_bwd_workspace_bytes(plan, q, k), dtype=torch.uint8, device="cuda")
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            lb.libra_attn_pool_fwd(q, k, v, plan, out=out, lse=lse)
+            lb.libra_attn_pool_bwd(q, k, v, out, lse, dout, plan, *grads, workspace=ws)
+        keep = q.clone()
+        q.neg_()
+        graph.replay()
+        q.copy_(keep)
+        graph.replay()
+    torch.cuda.synchronize()
+    assert same(a, (out, lse, grads))
+    del graph
+    plan.destroy()
+
+
+def test_noalloc_backward_follows_the_plan():
+    from paper_2607_23250_b200 import binding as lb
+    cu = pools.cu_seqlens([500, 300])
+    q, k, v, dout = _tensors(cu, 2, 1, 64, 8)
+    plan = _plan(cu, 2, 1, False, 90, 3)
+    out, lse, grads = _run(plan, q, k, v, dout, False)
+    mine = [torch.empty_like(x) for x in (q, k, v)]
+    lb.libra_attn_pool_bwd_noalloc(q, k, v, out, lse, dout, plan, *mine)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(grads, mine))
+    plan.destroy()
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_stalled_producers_give_up_cleanly(d):
+    """The bounded waits of the kernels with sinks, as in the tests of the others: no loads are issued, the launch reports a
+    timeout and the next one is right."""
+    from paper_2607_23250_b200 import binding as lb
+    lengths = [1200, 100]
+    cu = pools.cu_seqlens(lengths)
+    q, k, v, dout = _tensors(cu, 2, 1, d, 4)
+    plan = _plan(cu, 2, 1, False, 150, 4)
+    good = _run(plan, q, k, v, dout, False)
+    plan.set_wait_limit_ns(200_000)
+    plan.inject_stall(True)
+    lb.libra_attn_pool_fwd(q, k, v, plan)
+    with pytest.raises(lb.LibraError) as err:
+        plan.busy_times(lb.KERNEL_FWD)
+    assert err.value.code == lb.ERR_TIMEOUT
+    lb.libra_attn_pool_bwd(q, k, v, *good[:2], dout, plan)
+    with pytest.raises(lb.LibraError) as err:
+        plan.busy_times(lb.KERNEL_BWD_DQ)
+    assert err.value.code == lb.ERR_TIMEOUT
+    plan.inject_stall(False)
+    plan.set_wait_limit_ns(0)
+    again = _run(plan, q, k, v, dout, False)
+    assert torch.equal(good[0], again[0]) and all(torch.equal(x, y) for x, y in zip(good[2], again[2]))
+    plan.destroy()
