@@ -276,6 +276,41 @@ int libra_attn_pool_bwd_noalloc(const void* q_dev, const void* k_dev, const void
                                 void* dq_dev, void* dk_dev, void* dv_dev,
                                 const libra_dims* dims, void* stream);
 
+/* ---- activation checkpoints in 8 bits ------------------------------------------------------
+ * What a layer's backward pass reads of its forward pass (no counterpart in the paper: an aid to long contexts, where
+ * these tensors are most of what a layer keeps): q, k, v and out, held in 33 instead of 64 bytes per 32 values.
+ * Every run of 32 values along the head dimension shares an exponent byte E = max(bf16 exponent field of its largest magnitude,
+ * 7); a value x is the int8 rint(x * 2^(133 - E)), ties to even, at most 127 in magnitude, and stands for that integer times
+ * 2^(E - 133), which is a bf16 number.  So a value that is read back is off by half a step at most, 2^(E - 134); E = 255
+ * marks a run with an infinity or a NaN in it, all of which reads as NaN.  lse stays in fp32.
+ *   values [T, H, d] int8, exponents [T, H, d / 32] bytes, both contiguous; values aligned to 16 bytes. */
+typedef struct {
+    int8_t  *q, *k, *v, *out;
+    uint8_t *q_exp, *k_exp, *v_exp, *out_exp;
+} libra_ckpt8;
+
+/* Writes the checkpoint of the given tensors; unpack reads them back as bf16.  A tensor whose pointer (the bf16 one) is null is
+ * left out, and so may its checkpoint be.  Of dims, total_tokens, hq (q, out), hkv (k, v) and head_dim count.  One launch, no
+ * scratch; the tensors and the checkpoint do not overlap.  `ckpt` is a HOST struct of device pointers, read before the
+ * call returns.  Errors: INVALID_ARG (also misaligned tensors or values, or a tensor without its checkpoint), UNSUPPORTED
+ * (head_dim), OVERFLOW, CUDA. */
+int libra_ckpt8_pack(const void* q_dev, const void* k_dev, const void* v_dev, const void* out_dev,
+                     const libra_ckpt8* ckpt, const libra_dims* dims, void* stream);
+int libra_ckpt8_unpack(const libra_ckpt8* ckpt, void* q_dev, void* k_dev, void* v_dev, void* out_dev,
+                       const libra_dims* dims, void* stream);
+
+/* libra_attn_pool_bwd of the tensors that a checkpoint stands for, with any plan: the results are those of
+ * libra_ckpt8_unpack followed by libra_attn_pool_bwd (bit for bit in the two-kernel form), but out is never written
+ * out in bf16: the row statistics read it from the checkpoint.  q, k and v are restored into the workspace, which
+ * takes libra_attn_pool_bwd_ckpt8_workspace_bytes (0 on bad arguments), 256-byte aligned.  dq_dev may be dout_dev; otherwise
+ * the outputs overlap nothing that the call reads.  All tensors of the checkpoint are needed.
+ * Errors: those of libra_attn_pool_bwd, INVALID_ARG also for a checkpoint with a null or misaligned pointer. */
+size_t libra_attn_pool_bwd_ckpt8_workspace_bytes(const libra_plan_t* plan, const libra_dims* dims);
+int libra_attn_pool_bwd_ckpt8(const libra_ckpt8* ckpt, const float* lse_dev, const void* dout_dev,
+                              const int32_t* cu_seqlens_dev, const libra_plan_t* plan,
+                              void* dq_dev, void* dk_dev, void* dv_dev, void* workspace_dev,
+                              const libra_dims* dims, void* stream);
+
 /* ---- Variance-Reduced Sequence Placement (Section 4.2, Algorithm 1) ----------------------
  * Groups the D packed sequences of one optimizer-step window into K = D / P pools of exactly P
  * sequences with even summed attention work.  The paper runs it on a CPU core in the data path;

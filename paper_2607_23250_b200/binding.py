@@ -7,6 +7,7 @@ no CPU fallback.
 """
 from __future__ import annotations
 
+import collections
 import ctypes
 import os
 
@@ -29,6 +30,7 @@ ERR_SCRATCH_TOO_SMALL = -9
 EXPORTS = ["libra_plan_tiles", "libra_plan_tiles_window", "libra_plan_info", "libra_plan_status", "libra_plan_export",
            "libra_plan_export_pairs", "libra_plan_fused_ctas", "libra_plan_destroy", "libra_attn_pool_fwd", "libra_attn_pool_bwd_workspace_bytes",
            "libra_attn_pool_bwd", "libra_attn_pool_bwd_noalloc_max_bytes", "libra_attn_pool_bwd_noalloc",
+           "libra_ckpt8_pack", "libra_ckpt8_unpack", "libra_attn_pool_bwd_ckpt8_workspace_bytes", "libra_attn_pool_bwd_ckpt8",
            "libra_tap_schedule", "libra_busy_times", "libra_tile_times", "libra_plan_set_wait_limit_ns", "libra_plan_inject_stall", "libra_plan_set_timing", "libra_kernel_time_ms", "libra_kernel_times_ms", "libra_selftest_wait_timeout", "libra_launch_count",
            "libra_strerror"]
 
@@ -45,7 +47,15 @@ class Dims(ctypes.Structure):
                 ("hkv", ctypes.c_int), ("head_dim", ctypes.c_int), ("softmax_scale", ctypes.c_float)]
 
 
+class _Ckpt8Pointers(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v", "out", "q_exp", "k_exp", "v_exp", "out_exp")]
+
+
+# An 8-bit checkpoint: int8 values [T, H, d] and exponent bytes (uint8) [T, H, d / 32] of each tensor, or None.
+Ckpt8 = collections.namedtuple("Ckpt8", "q k v out q_exp k_exp v_exp out_exp", defaults=[None] * 8)
+
 _lib.libra_strerror.restype = ctypes.c_char_p
+_lib.libra_attn_pool_bwd_ckpt8_workspace_bytes.restype = ctypes.c_size_t
 _lib.libra_launch_count.restype = ctypes.c_int64
 _lib.libra_attn_pool_bwd_workspace_bytes.restype = ctypes.c_size_t
 _lib.libra_attn_pool_bwd_noalloc_max_bytes.restype = ctypes.c_size_t
@@ -256,6 +266,88 @@ def libra_attn_pool_bwd_noalloc(q, k, v, out, lse, dout, plan: Plan, dq, dk, dv,
     _check(_lib.libra_attn_pool_bwd_noalloc(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), _ptr(dout),
                                             _ptr(plan.cu_seqlens), plan._h, _ptr(dq), _ptr(dk), _ptr(dv),
                                             ctypes.byref(dims), _stream(stream)), "libra_attn_pool_bwd_noalloc")
+    return dq, dk, dv
+
+
+def _ckpt8_args(ckpt):
+    """Checks a checkpoint's tensors against one another -> pointers, dims (heads of 1 where it has no tensor with them)."""
+    shape = {}
+    for name in ("q", "k", "v", "out"):
+        val, exp = getattr(ckpt, name), getattr(ckpt, name + "_exp")
+        if val is None:
+            assert exp is None, f"{name}_exp without {name}"
+            continue
+        assert val.dtype == torch.int8 and exp is not None and exp.dtype == torch.uint8
+        for t in (val, exp):
+            assert t.is_cuda and t.is_contiguous() and t.dim() == 3, "expected contiguous 3-D CUDA tensors"
+            assert t.device.index == torch.cuda.current_device(), "tensor on another device than the current one"
+        T, h, d = val.shape
+        assert exp.shape == (T, h, d // 32)
+        for key, n in (("T", T), ("d", d), ("hq" if name in ("q", "out") else "hkv", h)):
+            assert shape.setdefault(key, n) == n, f"{name}: shapes do not match"
+    assert shape, "an empty checkpoint"
+    c = _Ckpt8Pointers(*(None if t is None else t.data_ptr() for t in ckpt))
+    return c, Dims(shape["T"], 0, shape.get("hq", 1), shape.get("hkv", 1), shape["d"], 0.0)
+
+
+def libra_ckpt8_pack(q=None, k=None, v=None, out=None, ckpt: Ckpt8 = None, stream=None) -> Ckpt8:
+    """8-bit checkpoint of the bf16 tensors given (q, out [T, Hq, d], k, v [T, Hkv, d]); into `ckpt` when that is given."""
+    xs = (q, k, v, out)
+    for x in xs:
+        assert x is None or (x.is_cuda and x.is_contiguous() and x.dtype == torch.bfloat16 and x.dim() == 3)
+        assert x is None or x.device.index == torch.cuda.current_device(), "tensor on another device than the current one"
+    if ckpt is None:
+        held = [None if x is None else torch.empty_like(x, dtype=torch.int8) for x in xs]
+        exps = [None if x is None else torch.empty((*x.shape[:2], x.shape[2] // 32), dtype=torch.uint8, device=x.device)
+                for x in xs]
+        ckpt = Ckpt8(*held, *exps)
+    c, dims = _ckpt8_args(ckpt)
+    for x, val in zip(xs, ckpt[:4]):
+        assert x is None or (val is not None and val.shape == x.shape), "the checkpoint has another shape"
+    _check(_lib.libra_ckpt8_pack(*(_ptr(x) for x in xs), ctypes.byref(c), ctypes.byref(dims), _stream(stream)),
+           "libra_ckpt8_pack")
+    return ckpt
+
+
+def libra_ckpt8_unpack(ckpt: Ckpt8, q=None, k=None, v=None, out=None, stream=None):
+    """(q, k, v, out) as bf16, into the tensors given, None for those that the checkpoint does not hold."""
+    c, dims = _ckpt8_args(ckpt)
+    xs = [None if val is None else (torch.empty_like(val, dtype=torch.bfloat16) if x is None else x)
+          for x, val in zip((q, k, v, out), ckpt[:4])]
+    for x, val in zip(xs, ckpt[:4]):
+        assert x is None or (x.dtype == torch.bfloat16 and x.is_contiguous() and x.shape == val.shape and x.device == val.device)
+    _check(_lib.libra_ckpt8_unpack(ctypes.byref(c), *(_ptr(x) for x in xs), ctypes.byref(dims), _stream(stream)),
+           "libra_ckpt8_unpack")
+    return tuple(xs)
+
+
+def _ckpt8_dims(ckpt, plan, scale):
+    c, dims = _ckpt8_args(ckpt)
+    assert all(t is not None for t in ckpt), "the backward pass needs q, k, v and out"
+    dims.n_samples = plan.cu_seqlens.numel() - 1
+    dims.softmax_scale = 0.0 if scale is None else float(scale)
+    return c, dims
+
+
+def libra_attn_pool_bwd_ckpt8_workspace_bytes(plan: Plan, ckpt: Ckpt8) -> int:
+    return int(_lib.libra_attn_pool_bwd_ckpt8_workspace_bytes(plan._h, ctypes.byref(_ckpt8_dims(ckpt, plan, None)[1])))
+
+
+def libra_attn_pool_bwd_ckpt8(ckpt: Ckpt8, lse, dout, plan: Plan, dq=None, dk=None, dv=None, workspace=None, scale=None,
+                              stream=None):
+    """Backward of the tensors that `ckpt` stands for -> dq, dk, dv."""
+    c, dims = _ckpt8_dims(ckpt, plan, scale)
+    _chk(lse, dout)
+    assert dout.dtype == torch.bfloat16 and dout.shape == ckpt.q.shape
+    assert lse.dtype == torch.float32 and lse.shape == (dims.hq, dims.total_tokens)
+    new = lambda like: torch.empty(like.shape, dtype=torch.bfloat16, device=like.device)  # noqa: E731
+    dq, dk, dv = new(ckpt.q) if dq is None else dq, new(ckpt.k) if dk is None else dk, new(ckpt.v) if dv is None else dv
+    _chk(dq, dk, dv)
+    if workspace is None:
+        workspace = torch.empty(libra_attn_pool_bwd_ckpt8_workspace_bytes(plan, ckpt), dtype=torch.uint8, device=dout.device)
+    _check(_lib.libra_attn_pool_bwd_ckpt8(ctypes.byref(c), _ptr(lse), _ptr(dout), _ptr(plan.cu_seqlens), plan._h, _ptr(dq),
+                                          _ptr(dk), _ptr(dv), _ptr(workspace), ctypes.byref(dims), _stream(stream)),
+           "libra_attn_pool_bwd_ckpt8")
     return dq, dk, dv
 
 

@@ -29,6 +29,7 @@
 //   S  = Q K^T   dP = dO V^T   dS = P o (dP - D) -> bf16 over dP   dQ += dS K     (every A operand in TMEM)
 #include <math.h>
 
+#include "ckpt8.cuh"
 #include "common.h"
 #include "ptx.cuh"
 
@@ -664,8 +665,10 @@ constexpr int kPrepRows = 8 * 256 / D;
 // Readers and clearers: of the first `spread` CTAs every period-th is of the rarer kind.
 struct PrepMix { uint32_t period, spread, clear_is_rare; };
 constexpr int64_t kPrepManyWarps = 24576;
-template <int D>
-__global__ void k_bwd_prep(const __nv_bfloat16* __restrict__ out, const __nv_bfloat16* __restrict__ dout,
+// HELD: out from a checkpoint, its integers and exponents.  A lane's eight values lie in one run, so its sum is scaled once;
+// by a power of two, so that it is bit for bit the sum over the values read back.
+template <int D, bool HELD>
+__global__ void k_bwd_prep(const void* __restrict__ out_, const uint8_t* __restrict__ out_exp, const __nv_bfloat16* __restrict__ dout,
                            const float* __restrict__ lse, int64_t T, int64_t Tpad, int hq, float* __restrict__ dvec,
                            float* __restrict__ lse2, float4* __restrict__ clear, int64_t n_clear, PrepMix mix, int rounds) {
     grid_dep_wait();
@@ -691,13 +694,23 @@ __global__ void k_bwd_prep(const __nv_bfloat16* __restrict__ out, const __nv_bfl
     for (int round = 0; round < rounds; ++round) {
         const int64_t t0 = ((int64_t)(w % groups) * rounds + round) * ROWS;
         float mine = 0.f;
-        uint4 a[STEPS], b[STEPS];
+        uint4 a[STEPS], b[STEPS];   // (HELD: two words of a are used)
+        uint32_t e[HELD ? STEPS : 1];
 #pragma unroll
         for (int u = 0; u < STEPS; ++u) {
             const int64_t t = t0 + u * RPS + sub;
             a[u] = b[u] = make_uint4(0, 0, 0, 0);
+            if (HELD) e[u % (HELD ? STEPS : 1)] = 7;
             if (t < T) {
-                a[u] = __ldg(reinterpret_cast<const uint4*>(out + ((size_t)t * hq + h) * D) + part);
+                if constexpr (HELD) {
+                    const size_t row = (size_t)t * hq + h;
+                    const uint2 x = __ldg(reinterpret_cast<const uint2*>(static_cast<const int8_t*>(out_) + row * D) + part);
+                    a[u].x = x.x;
+                    a[u].y = x.y;
+                    e[u] = __ldg(out_exp + row * (D / kRun) + part / (kRun / 8));
+                } else {
+                    a[u] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(out_) + ((size_t)t * hq + h) * D) + part);
+                }
                 b[u] = __ldg(reinterpret_cast<const uint4*>(dout + ((size_t)t * hq + h) * D) + part);
             }
         }
@@ -706,12 +719,19 @@ __global__ void k_bwd_prep(const __nv_bfloat16* __restrict__ out, const __nv_bfl
             const uint32_t* x = reinterpret_cast<const uint32_t*>(&a[u]);
             const uint32_t* y = reinterpret_cast<const uint32_t*>(&b[u]);
             float acc = 0.f;
+            float held[8];
+            if constexpr (HELD) {
+                held_floats(x[0], held);
+                held_floats(x[1], held + 4);
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float2 fa = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x[i]));
+                const float2 fa = HELD ? make_float2(held[2 * i], held[2 * i + 1])
+                                       : __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x[i]));
                 const float2 fb = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&y[i]));
                 acc += fa.x * fb.x + fa.y * fb.y;
             }
+            if constexpr (HELD) acc *= run_up(e[u]);
 #pragma unroll
             for (int off = LPR / 2; off > 0; off >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, off);
             // row u * RPS + sub of the warp's goes to the lane of that number
@@ -795,8 +815,9 @@ static int launch_bwd(const CUtensorMap& tq, const CUtensorMap& tk, const CUtens
 }
 
 // Row statistics; `clear` (16-byte words) is zeroed on the way: one pass over memory less to launch.
+struct RowsOut { const void* bf16; const libra_ckpt8* held; };   // one of the two
 template <int D>
-static cudaError_t launch_prep(const void* out, const void* dout, const float* lse, int64_t T, int64_t Tpad, int hq, float* dvec,
+static cudaError_t launch_prep(const RowsOut& out, const void* dout, const float* lse, int64_t T, int64_t Tpad, int hq, float* dvec,
                                float* lse2, float* clear, size_t clear_bytes, int sms, cudaStream_t s) {
     const int64_t n_clear = (int64_t)(clear_bytes / 16), runs = Tpad / kPrepRows<D> * hq;
     const int rounds = runs >= 4 * kPrepManyWarps ? 4 : (runs > 2 * 8 * ((int64_t)sms - 1) ? 2 : 1);
@@ -808,7 +829,8 @@ static cudaError_t launch_prep(const void* out, const void* dout, const float* l
     mix.period = (uint32_t)(rare ? usual / rare + 1 : 1);
     mix.spread = (uint32_t)(rare * mix.period);
     count_launch();
-    return launch_dependent(k_bwd_prep<D>, (unsigned)(readers + clearers), 256u, 0, s, (const __nv_bfloat16*)out,
+    return launch_dependent(out.held ? k_bwd_prep<D, true> : k_bwd_prep<D, false>, (unsigned)(readers + clearers), 256u, 0, s,
+                            out.held ? (const void*)out.held->out : out.bf16, out.held ? (const uint8_t*)out.held->out_exp : nullptr,
                             (const __nv_bfloat16*)dout, lse, T, Tpad, hq, dvec, lse2, (float4*)clear, n_clear, mix, rounds);
 }
 
@@ -925,13 +947,22 @@ static int launch_fused(const void* q_dev, const void* k_dev, const void* v_dev,
     return e == cudaSuccess ? LIBRA_OK : LIBRA_ERR_CUDA;
 }
 
-extern "C" int libra_attn_pool_bwd(const void* q_dev, const void* k_dev, const void* v_dev, const void* out_dev,
-                                   const float* lse_dev, const void* dout_dev, const int32_t* cu_seqlens_dev,
-                                   const libra_plan_t* plan, void* dq_dev, void* dk_dev, void* dv_dev,
-                                   void* workspace_dev, const libra_dims* dims, void* stream) {
-    if (!q_dev || !k_dev || !v_dev || !out_dev || !lse_dev || !dout_dev || !cu_seqlens_dev || !plan || !dq_dev ||
-        !dk_dev || !dv_dev || !workspace_dev || !dims)
-        return LIBRA_ERR_INVALID_ARG;
+// q, k, v restored from a checkpoint, behind the backward's own workspace.
+struct RestoredQkv { size_t q, k, v, total; };
+static RestoredQkv restored_qkv(size_t own, const libra_dims* dims) {
+    auto bytes = [&](int heads) { return ((size_t)dims->total_tokens * heads * dims->head_dim * 2 + 255) & ~(size_t)255; };
+    RestoredQkv r;
+    r.q = own;
+    r.k = r.q + bytes(dims->hq);
+    r.v = r.k + bytes(dims->hkv);
+    r.total = r.v + bytes(dims->hkv);
+    return r;
+}
+
+// held: q, k, v and out come from a checkpoint, q_dev, k_dev and v_dev are null.
+static int backward(const void* q_dev, const void* k_dev, const void* v_dev, const RowsOut& out, const float* lse_dev,
+                    const void* dout_dev, const libra_plan_t* plan, void* dq_dev, void* dk_dev, void* dv_dev, void* workspace_dev,
+                    const libra_dims* dims, void* stream) {
     if (dims->hq <= 0 || dims->hkv <= 0 || dims->hq % dims->hkv) return LIBRA_ERR_INVALID_ARG;
     if (dims->head_dim != 64 && dims->head_dim != 128 && dims->head_dim != 256) return LIBRA_ERR_UNSUPPORTED;
     const PlanDir& dq_dir = plan->dir[0];
@@ -951,8 +982,10 @@ extern "C" int libra_attn_pool_bwd(const void* q_dev, const void* k_dev, const v
         if (dims->hq % dq_dir.H) return LIBRA_ERR_INVALID_ARG;
         if (dkv_dir.W > plan->sm_count || dq_dir.W > plan->sm_count) return LIBRA_ERR_UNSUPPORTED;
     }
-    if (((uintptr_t)q_dev | (uintptr_t)k_dev | (uintptr_t)v_dev | (uintptr_t)out_dev | (uintptr_t)dout_dev |
+    if (((uintptr_t)q_dev | (uintptr_t)k_dev | (uintptr_t)v_dev | (uintptr_t)out.bf16 | (uintptr_t)dout_dev |
          (uintptr_t)dq_dev | (uintptr_t)dk_dev | (uintptr_t)dv_dev) & 15)
+        return LIBRA_ERR_INVALID_ARG;
+    if (const libra_ckpt8* c = out.held; c && (((uintptr_t)c->q | (uintptr_t)c->k | (uintptr_t)c->v | (uintptr_t)c->out) & 15))
         return LIBRA_ERR_INVALID_ARG;
     if ((uintptr_t)workspace_dev & 255) return LIBRA_ERR_INVALID_ARG;
     if (int rcd = check_plan_device(plan); rcd != LIBRA_OK) return rcd;
@@ -966,16 +999,25 @@ extern "C" int libra_attn_pool_bwd(const void* q_dev, const void* k_dev, const v
     if (s) const_cast<libra_plan_t*>(plan)->other_stream = 1;
 
     const float scale = dims->softmax_scale > 0.f ? dims->softmax_scale : 1.0f / sqrtf((float)D);
+    if (out.held) {
+        const RestoredQkv r = restored_qkv(ws.total, dims);
+        uint8_t* w = reinterpret_cast<uint8_t*>(workspace_dev);
+        time_begin(const_cast<libra_plan_t*>(plan), 3, s);
+        if (const int rc = launch_ckpt8_restore(out.held, w + r.q, w + r.k, w + r.v, dims, plan->d_status, s); rc != LIBRA_OK) return rc;
+        q_dev = w + r.q;
+        k_dev = w + r.k;
+        v_dev = w + r.v;
+    }
     if (D == 256) {   // row statistics, then the three passes of the 256-wide kernel
         libra_plan_t* mp256 = const_cast<libra_plan_t*>(plan);
-        time_begin(mp256, 3, s);
+        if (!out.held) time_begin(mp256, 3, s);
         float* dk_acc = nullptr;
         float* dv_acc = nullptr;
         if (fused) {
             dk_acc = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace_dev) + 2 * ws.stat_bytes);
             dv_acc = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace_dev) + 2 * ws.stat_bytes + ws.dkv_acc_bytes);
         }
-        const cudaError_t e256 = launch_prep<256>(out_dev, dout_dev, lse_dev, T, ws.Tpad, dims->hq, dvec, lse2, dk_acc,
+        const cudaError_t e256 = launch_prep<256>(out, dout_dev, lse_dev, T, ws.Tpad, dims->hq, dvec, lse2, dk_acc,
                                                   fused ? 2 * ws.dkv_acc_bytes : 0, plan->sm_count, s);
         time_end(mp256, 3, s);
         if (e256 != cudaSuccess) return LIBRA_ERR_CUDA;
@@ -1000,12 +1042,12 @@ extern "C" int libra_attn_pool_bwd(const void* q_dev, const void* k_dev, const v
     if (rc != LIBRA_OK) return rc;
 
     libra_plan_t* mp0 = const_cast<libra_plan_t*>(plan);
-    time_begin(mp0, 3, s);
+    if (!out.held) time_begin(mp0, 3, s);
     {
         float* acc = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace_dev) + 2 * ws.stat_bytes);
         const size_t acc_bytes = fused ? ws.dq_acc_bytes + 2 * ws.dkv_acc_bytes : 0;   // the three accumulators are contiguous
-        const cudaError_t e = D == 128 ? launch_prep<128>(out_dev, dout_dev, lse_dev, T, ws.Tpad, dims->hq, dvec, lse2, acc, acc_bytes, plan->sm_count, s)
-                                       : launch_prep<64>(out_dev, dout_dev, lse_dev, T, ws.Tpad, dims->hq, dvec, lse2, acc, acc_bytes, plan->sm_count, s);
+        const cudaError_t e = D == 128 ? launch_prep<128>(out, dout_dev, lse_dev, T, ws.Tpad, dims->hq, dvec, lse2, acc, acc_bytes, plan->sm_count, s)
+                                       : launch_prep<64>(out, dout_dev, lse_dev, T, ws.Tpad, dims->hq, dvec, lse2, acc, acc_bytes, plan->sm_count, s);
         if (e != cudaSuccess) return LIBRA_ERR_CUDA;
     }
     time_end(mp0, 3, s);
@@ -1067,4 +1109,29 @@ extern "C" int libra_attn_pool_bwd(const void* q_dev, const void* k_dev, const v
     libra_plan_t* mp = const_cast<libra_plan_t*>(plan);
     return D == 128 ? launch_bwd<128>(tq, tk, tv, tdo, tdq, pa, dkv_dir.W, share, pb, dq_dir.W, mp, s)
                     : launch_bwd<64>(tq, tk, tv, tdo, tdq, pa, dkv_dir.W, share, pb, dq_dir.W, mp, s);
+}
+
+extern "C" int libra_attn_pool_bwd(const void* q_dev, const void* k_dev, const void* v_dev, const void* out_dev,
+                                   const float* lse_dev, const void* dout_dev, const int32_t* cu_seqlens_dev,
+                                   const libra_plan_t* plan, void* dq_dev, void* dk_dev, void* dv_dev,
+                                   void* workspace_dev, const libra_dims* dims, void* stream) {
+    if (!q_dev || !k_dev || !v_dev || !out_dev || !lse_dev || !dout_dev || !cu_seqlens_dev || !plan || !dq_dev ||
+        !dk_dev || !dv_dev || !workspace_dev || !dims)
+        return LIBRA_ERR_INVALID_ARG;
+    return backward(q_dev, k_dev, v_dev, {out_dev, nullptr}, lse_dev, dout_dev, plan, dq_dev, dk_dev, dv_dev, workspace_dev, dims, stream);
+}
+
+extern "C" size_t libra_attn_pool_bwd_ckpt8_workspace_bytes(const libra_plan_t* plan, const libra_dims* dims) {
+    const size_t own = libra_attn_pool_bwd_workspace_bytes(plan, dims);
+    return own && plan->T == dims->total_tokens ? restored_qkv(own, dims).total : 0;
+}
+
+extern "C" int libra_attn_pool_bwd_ckpt8(const libra_ckpt8* ckpt, const float* lse_dev, const void* dout_dev,
+                                         const int32_t* cu_seqlens_dev, const libra_plan_t* plan, void* dq_dev, void* dk_dev,
+                                         void* dv_dev, void* workspace_dev, const libra_dims* dims, void* stream) {
+    if (!ckpt || !lse_dev || !dout_dev || !cu_seqlens_dev || !plan || !dq_dev || !dk_dev || !dv_dev || !workspace_dev || !dims)
+        return LIBRA_ERR_INVALID_ARG;
+    if (!ckpt->q || !ckpt->k || !ckpt->v || !ckpt->out || !ckpt->q_exp || !ckpt->k_exp || !ckpt->v_exp || !ckpt->out_exp)
+        return LIBRA_ERR_INVALID_ARG;
+    return backward(nullptr, nullptr, nullptr, {nullptr, ckpt}, lse_dev, dout_dev, plan, dq_dev, dk_dev, dv_dev, workspace_dev, dims, stream);
 }

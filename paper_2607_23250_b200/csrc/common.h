@@ -115,6 +115,8 @@ namespace libra {
 int make_thd_map(CUtensorMap* m, const void* base, int64_t T, int H, int d, int box_rows);
 // fp32 tensor [T, H, d] viewed as (d, H, T); box = box_cols x 1 x box_rows, 128-byte swizzle.
 int make_f32_3d_map(CUtensorMap* m, const void* base, int64_t T, int H, int d, int box_cols, int box_rows);
+// q, k, v of a checkpoint as bf16 (ckpt8.cu); nothing where *plan_status is not 0.
+int launch_ckpt8_restore(const libra_ckpt8* c, void* q, void* k, void* v, const libra_dims* dims, const int* plan_status, cudaStream_t s);
 // head_dim 256 (attn_d256.cu): the forward over the plan's query-major lists; the three gradient passes over
 // its key-major (dV, dK) and query-major (dQ) lists, given the row statistics lse2 / dvec [Hq, Tpad].
 int launch_fwd_d256(const void* q, const void* k, const void* v, void* out, float* lse, const libra_plan* plan,

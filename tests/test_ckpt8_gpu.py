@@ -1,0 +1,201 @@
+"""8-bit activation checkpoints on the GPU: the format bit for bit, and the backward pass out of them."""
+import numpy as np
+import pytest
+import torch
+
+import ckpt_reference as ref
+import window_reference as wref
+from paper_2607_23250_b200 import pools
+
+pytestmark = pytest.mark.gpu
+
+# infinities, NaN, zeros, subnormals, ties, runs of one large value, the largest and smallest numbers
+def _values(shape, seed):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(shape, generator=g) * torch.exp2(torch.randint(-20, 20, (*shape[:2], 1), generator=g).float())
+    x = x.to(torch.bfloat16)
+    flat = x.view(-1, 32)
+    odd = [float("inf"), -float("inf"), float("nan"), 0.0, -0.0, 2.0 ** -133, -2.0 ** -127, 3.3895313892515355e38, 127.5, -127.5, 0.5, 1.5, 2.5]
+    for i in range(min(len(flat), 4 * len(odd))):
+        if i % 4 == 1:
+            flat[i, (7 * i) % 32] = odd[i // 4]
+        if i % 4 == 2:
+            flat[i] = odd[i // 4]
+        if i % 4 == 3:                                     # steps of one: ties at .5
+            flat[i] = torch.arange(32) * 0.5 + 48
+            flat[i, 0] = odd[8 + (i // 4) % 5]
+    return x
+
+
+def _bits(x):
+    return x.contiguous().view(torch.int16).cpu()
+
+
+@pytest.mark.parametrize("T,hq,hkv,d", [(1, 1, 1, 64), (1, 3, 1, 128), (5, 3, 1, 64), (7, 2, 2, 256), (33, 1, 1, 64), (129, 5, 1, 128), (1000, 8, 2, 128)])
+def test_pack_and_unpack_match_the_definition(T, hq, hkv, d):
+    from paper_2607_23250_b200 import binding as lb
+    xs = [_values((T, h, d), 10 * T + i) for i, h in enumerate((hq, hkv, hkv, hq))]
+    ckpt = lb.libra_ckpt8_pack(*(x.cuda() for x in xs))
+    back = lb.libra_ckpt8_unpack(ckpt)
+    for x, q, e, y in zip(xs, ckpt[:4], ckpt[4:], back):
+        want_q, want_e = ref.held(x)
+        assert np.array_equal(e.cpu().numpy(), want_e)
+        fine = np.repeat(want_e != 255, 32, -1)
+        assert np.array_equal(q.cpu().numpy()[fine], want_q[fine])
+        want = ref.value(want_q, want_e)
+        got = y.double().cpu().numpy()
+        assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[fine], want[fine])
+
+
+def test_parts_of_a_layer_and_tensors_given():
+    from paper_2607_23250_b200 import binding as lb
+    k = torch.randn((70, 2, 64), dtype=torch.bfloat16, device="cuda")
+    out = torch.randn((70, 6, 64), dtype=torch.bfloat16, device="cuda")
+    ckpt = lb.libra_ckpt8_pack(k=k, out=out)
+    assert ckpt.q is None and ckpt.v is None and ckpt.k.shape == k.shape and ckpt.out_exp.shape == (70, 6, 2)
+    q, k2, v, out2 = lb.libra_ckpt8_unpack(ckpt)
+    assert q is None and v is None
+    # into memory at hand, whose neighbours stay as they are
+    room = torch.full((80, 2, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    held = torch.full((80, 2, 64), 5, dtype=torch.int8, device="cuda")
+    exps = torch.full((80, 2, 2), 9, dtype=torch.uint8, device="cuda")
+    lb.libra_ckpt8_pack(k=k, ckpt=lb.Ckpt8(k=held[5:75], k_exp=exps[5:75]))
+    lb.libra_ckpt8_unpack(lb.Ckpt8(k=held[5:75], k_exp=exps[5:75]), k=room[5:75])
+    assert torch.equal(room[5:75], k2) and torch.equal(held[5:75], ckpt.k) and torch.equal(exps[5:75], ckpt.k_exp)
+    for x, fill in ((room, 7.0), (held, 5), (exps, 9)):
+        assert bool((x[:5] == fill).all()) and bool((x[75:] == fill).all())
+    with pytest.raises(AssertionError):
+        lb.libra_ckpt8_pack(k=k.transpose(0, 1))
+    with pytest.raises(AssertionError):
+        lb.libra_ckpt8_pack(k=k.float())
+    with pytest.raises(AssertionError):
+        lb.libra_ckpt8_pack(k=k, out=out[:60])
+    with pytest.raises(lb.LibraError) as err:
+        lb.libra_ckpt8_pack(k=torch.zeros((4, 1, 96), dtype=torch.bfloat16, device="cuda"))
+    assert err.value.code == lb.ERR_UNSUPPORTED
+
+
+LENGTHS = [150, 1, 700, 33, 260]
+
+
+def _layer(d, fused, window, sinks, lengths=LENGTHS, hq=4, hkv=2, seed=0, **kw):
+    from paper_2607_23250_b200 import binding as lb
+    cu = pools.cu_seqlens(lengths)
+    t = pools.make_tensors(int(cu[-1]), hq, hkv, d, seed=seed)
+    q, k, v, dout = (t[n].cuda() for n in ("q", "k", "v", "dout"))
+    directions = lb.LIBRA_DIR_Q | (lb.LIBRA_DIR_PAIR if fused else lb.LIBRA_DIR_KV)
+    plan = lb.libra_plan_tiles(torch.from_numpy(cu).cuda(), hq, 256, directions=directions, tile_kv=128, n_heads_kv=hkv,
+                               window=window, sinks=sinks, **kw)
+    out, lse = lb.libra_attn_pool_fwd(q, k, v, plan)
+    return cu, plan, (q, k, v, out), lse, dout
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 0), (130, 5)])
+@pytest.mark.parametrize("d,fused", [(64, False), (128, False), (128, True), (256, False), (256, True)])
+def test_backward_out_of_a_checkpoint(d, fused, window, sinks):
+    """Against the gradients of the tensors that the checkpoint stands for, in 64 bits; in the two-kernel form also the
+    same bits as reading it back first."""
+    from paper_2607_23250_b200 import binding as lb
+    cu, plan, xs, lse, dout = _layer(d, fused, window, sinks, seed=d + window)
+    ckpt = lb.libra_ckpt8_pack(*xs)
+    grads = lb.libra_attn_pool_bwd_ckpt8(ckpt, lse, dout, plan)
+    torch.cuda.synchronize()
+    plan.busy_times(lb.KERNEL_BWD_FUSED if fused and d == 128 else lb.KERNEL_BWD_DQ)
+    vals = [torch.from_numpy(ref.value(q.cpu().numpy(), e.cpu().numpy())).cuda() for q, e in zip(ckpt[:4], ckpt[4:])]
+    see = wref.visible(cu, window, sinks, "cuda")
+    want, bounds = wref.backward(*vals, lse, dout, see)
+    for name, g, w, b in zip(("dq", "dk", "dv"), grads, want, bounds):
+        assert wref.worst(g, w, b) <= 1, name
+    back = lb.libra_ckpt8_unpack(ckpt)
+    again = lb.libra_attn_pool_bwd(*back, lse, dout, plan)
+    if not fused:
+        assert all(torch.equal(x, y) for x, y in zip(grads, again))
+    plan.destroy()
+
+
+def test_backward_on_pairs_of_ctas_and_over_dout():
+    """The fused form on pairs of CTAs; dq written over dout."""
+    from paper_2607_23250_b200 import binding as lb
+    cu, plan, xs, lse, dout = _layer(128, True, 0, 0, lengths=[1100], pair_chunk=512)
+    assert plan.fused_ctas() == 2
+    ckpt = lb.libra_ckpt8_pack(*xs)
+    vals = [torch.from_numpy(ref.value(q.cpu().numpy(), e.cpu().numpy())).cuda() for q, e in zip(ckpt[:4], ckpt[4:])]
+    want, bounds = wref.backward(*vals, lse, dout, wref.visible(cu, 0, 0, "cuda"))
+    for over in (False, True):
+        g = dout.clone()
+        grads = lb.libra_attn_pool_bwd_ckpt8(ckpt, lse, g, plan, dq=g if over else None)
+        for x, w, b in zip(grads, want, bounds):
+            assert wref.worst(x, w, b) <= 1
+    plan.destroy()
+
+
+def test_refusals_and_bad_plans_leave_the_outputs():
+    from paper_2607_23250_b200 import binding as lb
+    cu, plan, xs, lse, dout = _layer(128, False, 60, 2)
+    ckpt = lb.libra_ckpt8_pack(*xs)
+    size = lb.libra_attn_pool_bwd_ckpt8_workspace_bytes(plan, ckpt)
+    T = int(cu[-1])
+    assert size == lb.libra_attn_pool_bwd_workspace_bytes(plan, *xs[:2]) + 256 * (-(-T * 4 * 256 // 256) + 2 * -(-T * 2 * 256 // 256))
+    with pytest.raises(AssertionError):
+        lb.libra_attn_pool_bwd_ckpt8(ckpt._replace(out=None, out_exp=None), lse, dout, plan)
+    with pytest.raises(AssertionError):
+        lb.libra_attn_pool_bwd_ckpt8(ckpt, lse[:, :5].contiguous(), dout, plan)
+    ws = torch.empty(size + 16, dtype=torch.uint8, device="cuda")
+    with pytest.raises(lb.LibraError) as err:
+        lb.libra_attn_pool_bwd_ckpt8(ckpt, lse, dout, plan, workspace=ws[16:])
+    assert err.value.code == lb.ERR_INVALID_ARG
+    other = lb.libra_plan_tiles(torch.tensor([0, T - 1], dtype=torch.int32).cuda(), 4, 256, tile_kv=128, n_heads_kv=2)
+    with pytest.raises(lb.LibraError) as err:
+        lb.libra_attn_pool_bwd_ckpt8(ckpt, lse, dout, other, workspace=ws)
+    assert err.value.code == lb.ERR_PLAN_MISMATCH
+    bad = lb.libra_plan_tiles(torch.tensor([0, 50, 20, T], dtype=torch.int32).cuda(), 4, 256, tile_kv=128, n_heads_kv=2, total_tokens=T)
+    grads = [torch.full(x.shape, 7.0, dtype=torch.bfloat16, device="cuda") for x in xs[:3]]
+    lb.libra_attn_pool_bwd_ckpt8(ckpt, lse, dout, bad, *grads)
+    assert all(bool((g == 7).all()) for g in grads)
+    for p in (plan, other, bad):
+        p.destroy()
+
+
+def test_a_training_layer_captured_on_a_stream():
+    """Forward, checkpoint and backward of a windowed layer as one graph, replayed on new inputs."""
+    from paper_2607_23250_b200 import binding as lb
+    cu, plan, (q, k, v, out), lse, dout = _layer(128, False, 90, 3)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+
+    def layer(ws, ckpt, grads):
+        lb.libra_attn_pool_fwd(q, k, v, plan, out=out, lse=lse)
+        lb.libra_ckpt8_pack(q, k, v, out, ckpt=ckpt)
+        lb.libra_attn_pool_bwd_ckpt8(ckpt, lse, dout, plan, *grads, workspace=ws)
+
+    with torch.cuda.stream(side):
+        ckpt = lb.libra_ckpt8_pack(q, k, v, out)
+        ws = torch.empty(lb.libra_attn_pool_bwd_ckpt8_workspace_bytes(plan, ckpt), dtype=torch.uint8, device="cuda")
+        grads = [torch.empty_like(x) for x in (q, k, v)]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            layer(ws, ckpt, grads)
+        for step in range(2):
+            q.copy_(torch.roll(q, 1, 0))
+            graph.replay()
+            got = [x.clone() for x in (out, lse, *grads, *ckpt)]
+            layer(ws, ckpt, grads)
+            assert all(torch.equal(x, y) for x, y in zip(got, (out, lse, *grads, *ckpt)))
+    torch.cuda.synchronize()
+    del graph
+    plan.destroy()
+
+
+def test_kernel_times_and_launch_counts():
+    from paper_2607_23250_b200 import binding as lb
+    cu, plan, xs, lse, dout = _layer(128, True, 60, 2)
+    n0 = lb.launch_count()
+    ckpt = lb.libra_ckpt8_pack(*xs)
+    assert lb.launch_count() == n0 + 1
+    lb.libra_ckpt8_unpack(ckpt)
+    assert lb.launch_count() == n0 + 2
+    plan.set_timing(True)
+    lb.libra_attn_pool_bwd_ckpt8(ckpt, lse, dout, plan)
+    assert lb.launch_count() == n0 + 6                     # restoring, row statistics, fused, conversion
+    assert plan.kernel_time_ms(lb.KERNEL_BWD_PREP) > 0
+    plan.destroy()
