@@ -137,10 +137,14 @@ int libra_plan_tiles(const int32_t* cu_seqlens_dev, int n_samples, int n_heads, 
  * that is the last `window` positions, its own among them, and the first `sinks` of its sample.  The plan carries the
  * mask: libra_attn_pool_fwd, libra_attn_pool_bwd, libra_attn_pool_bwd_noalloc and libra_attn_pool_bwd_ckpt8 called with it
  * compute attention and gradients over those pairs, in every form and at every head_dim; key blocks that no row of a tile
- * sees are not read.  Tile weights count the visible pairs (LIBRA_WEIGHT_PAIRS) or the executed blocks
- * (LIBRA_WEIGHT_BLOCKS); the pair-blocks of a query chunk are the key blocks of which it sees a key: with sinks those that
- * hold the sinks of its first row's sample, then the others, ascending.
- * A window that is not below T, or not below any sample's length, gives what libra_plan_tiles gives.  As there, an infinity or
+ * sees are not read.  Tile weights are block counts (LIBRA_WEIGHT_BLOCKS) of the mask, with opts->weight_model =
+ * LIBRA_WEIGHT_PAIRS too, which then stands for cost_block 128 and unit costs of the library's own: by visible pairs the tiles'
+ * times would be far from their weights.  The pair-blocks of a query chunk are the key blocks of which it sees a key: with sinks those that
+ * hold the sinks of its first row's sample, then the others, ascending.  (With sinks the two-kernel backward at head_dim 64 and
+ * 128 walks lists of its own instead of the key-major ones, in which the row blocks beyond the window of a key block that
+ * holds sinks are tiles of their own; their partial sums are added up in a fixed order, in its workspace.)
+ * A window that is not below T gives what libra_plan_tiles gives, one that is not below any sample's length the same
+ * results (with sinks up to rounding).  As there, an infinity or
  * a NaN of a key or value reaches rows that do not see it where they share a 128-row block with rows, and a key
  * block with keys, that are seen.
  * Errors: INVALID_ARG (window < 1, sinks < 0), otherwise those of libra_plan_tiles. */

@@ -269,42 +269,71 @@ def libra_attn_pool_bwd_noalloc(q, k, v, out, lse, dout, plan: Plan, dq, dk, dv,
     return dq, dk, dv
 
 
-def _ckpt8_args(ckpt):
-    """Checks a checkpoint's tensors against one another -> pointers, dims (heads of 1 where it has no tensor with them)."""
-    shape = {}
-    for name in ("q", "k", "v", "out"):
-        val, exp = getattr(ckpt, name), getattr(ckpt, name + "_exp")
-        if val is None:
-            assert exp is None, f"{name}_exp without {name}"
+def _ckpt8_dims_of(tensors):
+    """dims of (q, k, v, out), each [T, H, *] or None; heads of 1 where there is no tensor with them."""
+    T = d = hq = hkv = None
+    here = torch.cuda.current_device()
+    for i, t in enumerate(tensors):
+        if t is None:
             continue
-        assert val.dtype == torch.int8 and exp is not None and exp.dtype == torch.uint8
-        for t in (val, exp):
-            assert t.is_cuda and t.is_contiguous() and t.dim() == 3, "expected contiguous 3-D CUDA tensors"
-            assert t.device.index == torch.cuda.current_device(), "tensor on another device than the current one"
-        T, h, d = val.shape
-        assert exp.shape == (T, h, d // 32)
-        for key, n in (("T", T), ("d", d), ("hq" if name in ("q", "out") else "hkv", h)):
-            assert shape.setdefault(key, n) == n, f"{name}: shapes do not match"
-    assert shape, "an empty checkpoint"
-    c = _Ckpt8Pointers(*(None if t is None else t.data_ptr() for t in ckpt))
-    return c, Dims(shape["T"], 0, shape.get("hq", 1), shape.get("hkv", 1), shape["d"], 0.0)
+        assert t.is_cuda and t.is_contiguous() and t.dim() == 3, "expected contiguous 3-D CUDA tensors"
+        assert t.device.index == here, "tensor on another device than the current one"
+        n, h, w = t.shape
+        heads = hkv if i in (1, 2) else hq
+        assert (T is None or (n, w) == (T, d)) and (heads is None or heads == h), "shapes do not match"
+        T, d = n, w
+        if i in (1, 2):
+            hkv = h
+        else:
+            hq = h
+    assert T is not None, "no tensor"
+    return Dims(T, 0, hq or 1, hkv or 1, d, 0.0)
+
+
+def _ckpt8_args(ckpt):
+    """Checks a checkpoint's tensors -> pointers, dims."""
+    dims = _ckpt8_dims_of(ckpt[:4])
+    T, w = dims.total_tokens, dims.head_dim // 32
+    for i in range(4):
+        val, exp = ckpt[i], ckpt[4 + i]
+        if val is None:
+            assert exp is None, "exponents without values"
+            continue
+        assert val.dtype is torch.int8 and exp is not None and exp.dtype is torch.uint8
+        assert exp.is_contiguous() and exp.device == val.device
+        assert exp.shape == (T, dims.hkv if i in (1, 2) else dims.hq, w), "exponents of another shape"
+    return _Ckpt8Pointers(*[None if t is None else t.data_ptr() for t in ckpt]), dims
+
+
+def _packed(shapes, dtype, device):
+    """Contiguous tensors of these shapes (None: none) in one allocation; every size is a multiple of 16 bytes but the last ones'.
+    (An allocation each costs more than the kernels of a small layer.)"""
+    sizes = [0 if x is None else x[0] * x[1] * x[2] for x in shapes]
+    room = torch.empty(sum(sizes), dtype=dtype, device=device)
+    at, out = 0, []
+    for x, n in zip(shapes, sizes):
+        out.append(None if x is None else room.as_strided(x, (x[1] * x[2], x[2], 1), at))
+        at += n
+    return out
 
 
 def libra_ckpt8_pack(q=None, k=None, v=None, out=None, ckpt: Ckpt8 = None, stream=None) -> Ckpt8:
-    """8-bit checkpoint of the bf16 tensors given (q, out [T, Hq, d], k, v [T, Hkv, d]); into `ckpt` when that is given."""
+    """8-bit checkpoint of the bf16 tensors given (q, out [T, Hq, d], k, v [T, Hkv, d]); into `ckpt` when that is given, else
+    into memory of its own, all of it one allocation."""
     xs = (q, k, v, out)
-    for x in xs:
-        assert x is None or (x.is_cuda and x.is_contiguous() and x.dtype == torch.bfloat16 and x.dim() == 3)
-        assert x is None or x.device.index == torch.cuda.current_device(), "tensor on another device than the current one"
+    assert all(x is None or x.dtype is torch.bfloat16 for x in xs)
+    dims = _ckpt8_dims_of(xs)
     if ckpt is None:
-        held = [None if x is None else torch.empty_like(x, dtype=torch.int8) for x in xs]
-        exps = [None if x is None else torch.empty((*x.shape[:2], x.shape[2] // 32), dtype=torch.uint8, device=x.device)
-                for x in xs]
-        ckpt = Ckpt8(*held, *exps)
-    c, dims = _ckpt8_args(ckpt)
-    for x, val in zip(xs, ckpt[:4]):
-        assert x is None or (val is not None and val.shape == x.shape), "the checkpoint has another shape"
-    _check(_lib.libra_ckpt8_pack(*(_ptr(x) for x in xs), ctypes.byref(c), ctypes.byref(dims), _stream(stream)),
+        d, device = dims.head_dim, next(x for x in xs if x is not None).device
+        shapes = [None if x is None else tuple(x.shape) for x in xs]
+        both = _packed(shapes + [x and (x[0], x[1], d // 32) for x in shapes], torch.int8, device)
+        ckpt = Ckpt8(*both[:4], *[x if x is None else x.view(torch.uint8) for x in both[4:]])
+        c = _Ckpt8Pointers(*[None if t is None else t.data_ptr() for t in ckpt])
+    else:
+        c, _ = _ckpt8_args(ckpt)
+        for x, val in zip(xs, ckpt):
+            assert x is None or (val is not None and val.shape == x.shape), "the checkpoint has another shape"
+    _check(_lib.libra_ckpt8_pack(*[_ptr(x) for x in xs], ctypes.byref(c), ctypes.byref(dims), _stream(stream)),
            "libra_ckpt8_pack")
     return ckpt
 
@@ -312,11 +341,15 @@ def libra_ckpt8_pack(q=None, k=None, v=None, out=None, ckpt: Ckpt8 = None, strea
 def libra_ckpt8_unpack(ckpt: Ckpt8, q=None, k=None, v=None, out=None, stream=None):
     """(q, k, v, out) as bf16, into the tensors given, None for those that the checkpoint does not hold."""
     c, dims = _ckpt8_args(ckpt)
-    xs = [None if val is None else (torch.empty_like(val, dtype=torch.bfloat16) if x is None else x)
-          for x, val in zip((q, k, v, out), ckpt[:4])]
-    for x, val in zip(xs, ckpt[:4]):
-        assert x is None or (x.dtype == torch.bfloat16 and x.is_contiguous() and x.shape == val.shape and x.device == val.device)
-    _check(_lib.libra_ckpt8_unpack(ctypes.byref(c), *(_ptr(x) for x in xs), ctypes.byref(dims), _stream(stream)),
+    xs = [q, k, v, out]
+    for x, val in zip(xs, ckpt):
+        assert x is None or (val is not None and x.dtype is torch.bfloat16 and x.is_contiguous() and x.shape == val.shape
+                             and x.device == val.device)
+    shapes = [tuple(val.shape) if x is None and val is not None else None for x, val in zip(xs, ckpt)]
+    if any(shapes):
+        new = _packed(shapes, torch.bfloat16, next(val for val in ckpt if val is not None).device)
+        xs = [y if x is None else x for x, y in zip(xs, new)]
+    _check(_lib.libra_ckpt8_unpack(ctypes.byref(c), *[_ptr(x) for x in xs], ctypes.byref(dims), _stream(stream)),
            "libra_ckpt8_unpack")
     return tuple(xs)
 

@@ -29,8 +29,10 @@
 //   S  = Q K^T   dP = dO V^T   dS = P o (dP - D) -> bf16 over dP   dQ += dS K     (every A operand in TMEM)
 #include <math.h>
 
-#include "ckpt8.cuh"
+#include <type_traits>
+
 #include "common.h"
+#include "ckpt8.cuh"
 #include "ptx.cuh"
 
 namespace libra {
@@ -78,8 +80,6 @@ struct DkvParams {
     const int32_t* cta_offsets;
     const int32_t* cta_tiles;
     const int32_t* tok_end;
-    const int32_t* blk_end;  // [ceil(T / 128)] largest tok_end of a block's keys, and a bound of them from below
-    const int32_t* blk_min;
     int64_t T, Tpad;
     int hq, hkv;
     float scale, scale_log2;
@@ -88,11 +88,26 @@ struct DkvParams {
     uint32_t wait_limit_ns;
     int inject_stall;        // test aid: the producer (SHARE: of odd ranks) issues no loads, so the consumers' waits run out
     uint64_t* busy;
+    const int2* blk;         // [ceil(T / 128)] of a block's keys at most the smallest tok_end, and the largest
+};
+
+// TAILS.  (Two more pointers in the other instances' arguments cost them registers: 92 bytes of spills read back instead of 48, 1 % of
+// a step on 4096 tokens with 4 heads of 64.)
+struct DkvTailParams : DkvParams {
+    const int4* units;       // key block, first row block, row blocks, slot of partial sums (-1: none)
+    float* partial;          // [slots][Hkv][dK, dV][128][D]
 };
 
 // Query blocks a key block [k0, k0+128) is seen by: diagonal .. block of the last query that sees one of its keys (without a
 // window and sinks the last one of its last key's sample).
-__device__ __forceinline__ int last_q_block(const int32_t* blk_end, int64_t k0) { return (blk_end[k0 / kBlk] - 1) / kBlk; }
+__device__ __forceinline__ int last_q_block(const int2* blk, int64_t k0) { return (blk[k0 / kBlk].y - 1) / kBlk; }
+
+// A tile of the list.
+__device__ __forceinline__ int4 dkv_unit(const DkvTailParams& p, int t) { return p.units[t / p.hkv]; }
+__device__ __forceinline__ int4 dkv_unit(const DkvParams& p, int t) {   // key block, first row block, row blocks, slot
+    const int j = t / p.hkv;
+    return make_int4(j, j, (p.blk[j].y - 1) / kBlk - j + 1, -1);
+}
 
 __device__ __forceinline__ void tmem_ld128(uint32_t taddr, uint32_t* r) {
     tmem_ld32(taddr, r);
@@ -176,11 +191,13 @@ __device__ __noinline__ bool finish_shared(uint8_t* smem, uint64_t* bar_spent, u
 // fewer tiles than SMs the longest, G heads times the blocks of its sample, is the launch.  Step with one CTA a tile and with several: 2000 tokens, 8 /
 // 2 heads of 64: 104.6 -> 65.8 us (4 CTAs); 4000 tokens in one sample, 4 / 1 heads of 128: 237.9 -> 146.4 (4); 1500 tokens, 4 /
 // 1 heads: 96.8 -> 60.4 (8); 9000 tokens: 236.9 -> 162.3 (2).
-template <int D, bool SHARE>
+// TAILS (plans with sinks, not shared): the units are those of direction 5 (k_tail_units in plan.cu); some leave partial sums
+// in fp32, which k_sum_tails adds up.
+template <int D, bool SHARE, bool TAILS>
 __global__ void __launch_bounds__(kBwdThreads, 1)
 k_attn_bwd_dkdv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                 const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_do,
-                const DkvParams p) {
+                const std::conditional_t<TAILS, DkvTailParams, DkvParams> p) {
     using L = DkvSmem<D>;
     constexpr int QS = L::kQStages, DS = L::kDoStages;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -277,9 +294,10 @@ k_attn_bwd_dkdv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             for (int idx = unit_begin; idx < unit_end && ok && !(p.inject_stall && (!SHARE || rank % 2 == 1)); ++idx) {
                 const int t = p.cta_tiles[idx];
                 const int kvh = t % p.hkv;
-                const int64_t k0 = (int64_t)(t / p.hkv) * kBlk;
-                const int i_lo = (int)(k0 / kBlk);
-                const int nblk = last_q_block(p.blk_end, k0) - i_lo + 1;
+                const int4 unit = dkv_unit(p, t);
+                const int64_t k0 = (int64_t)unit.x * kBlk;
+                const int i_lo = unit.y, nblk = unit.z;
+                if (TAILS && nblk == 0) continue;
                 const int it0 = SHARE ? share_begin(G * nblk, rank, size) : 0;
                 const int n_it = (SHARE ? share_begin(G * nblk, rank + 1, size) : G * nblk) - it0;
                 if (SHARE && n_it == 0) break;
@@ -363,10 +381,8 @@ k_attn_bwd_dkdv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 return true;
             };
             for (int idx = unit_begin; idx < unit_end && ok; ++idx) {
-                const int t = p.cta_tiles[idx];
-                const int64_t k0 = (int64_t)(t / p.hkv) * kBlk;
-                const int i_lo = (int)(k0 / kBlk);
-                const int nblk = last_q_block(p.blk_end, k0) - i_lo + 1;
+                const int nblk = dkv_unit(p, p.cta_tiles[idx]).z;
+                if (TAILS && nblk == 0) continue;
                 const int n_it = SHARE ? share_begin(G * nblk, rank + 1, size) - share_begin(G * nblk, rank, size) : G * nblk;
                 if (SHARE && n_it == 0) break;
                 ok = mbar_wait(bar_kvfull, ucnt & 1, abort_flag);
@@ -435,10 +451,7 @@ k_attn_bwd_dkdv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         uint32_t it_all = 0;
         bool ok = true;
         for (int idx = unit_begin; idx < unit_end && ok; ++idx) {
-            const int t = p.cta_tiles[idx];
-            const int64_t k0 = (int64_t)(t / p.hkv) * kBlk;
-            const int i_lo = (int)(k0 / kBlk);
-            const int nblk = last_q_block(p.blk_end, k0) - i_lo + 1;
+            const int nblk = dkv_unit(p, p.cta_tiles[idx]).z;
             const int n_it = SHARE ? share_begin(G * nblk, rank + 1, size) - share_begin(G * nblk, rank, size) : G * nblk;
             // ---- dS group: dS^T = P^T o (dP^T - D) ----
             for (int it = 0; it < n_it && ok; ++it, ++it_all) {
@@ -516,9 +529,10 @@ k_attn_bwd_dkdv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         for (int idx = unit_begin; idx < unit_end && ok; ++idx) {
             const int t = p.cta_tiles[idx];
             const int kvh = t % p.hkv;
-            const int64_t k0 = (int64_t)(t / p.hkv) * kBlk;
-            const int i_lo = (int)(k0 / kBlk);
-            const int nblk = last_q_block(p.blk_end, k0) - i_lo + 1;
+            const int4 unit = dkv_unit(p, t);
+            const int64_t k0 = (int64_t)unit.x * kBlk;
+            const int i_lo = unit.y, nblk = unit.z, slot = unit.w;
+            if (TAILS && nblk == 0) continue;
             const int it0 = SHARE ? share_begin(G * nblk, rank, size) : 0;
             const int n_it = (SHARE ? share_begin(G * nblk, rank + 1, size) : G * nblk) - it0;
             const int64_t key = k0 + r;
@@ -527,7 +541,7 @@ k_attn_bwd_dkdv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             const int c0 = 64 * grp;   // this group's query columns
             const uint64_t scale2 = f2_pack(p.scale_log2, p.scale_log2), neg1 = f2_pack(-1.f, -1.f);
             const int kend = key_ok ? p.tok_end[key] : 0;
-            const int min_kend = p.blk_min[k0 / kBlk];
+            const int min_kend = p.blk[k0 / kBlk].x;
             const bool partial = k0 + kBlk > p.T;
             for (int it = 0; it < n_it && ok; ++it, ++it_all) {
                 const int qb = (i_lo + (it0 + it) % nblk) * kBlk;
@@ -608,7 +622,15 @@ k_attn_bwd_dkdv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                     uint32_t v[32];
                     tmem_ld32((which == 0 ? t_dk : t_dv) + cc, v);
                     tmem_ld_wait();
-                    if (key_ok) {
+                    bool stored = false;
+                    if constexpr (TAILS) if (slot >= 0) {   // keys past the pool: zeros
+                        stored = true;
+                        float* dst = p.partial + ((((size_t)slot * p.hkv + kvh) * 2 + which) * 128 + r) * D + grp * kCols + cc;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4)
+                            *reinterpret_cast<uint4*>(dst + i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                    }
+                    if (key_ok && !stored) {
 #pragma unroll
                         for (int i = 0; i < 32; i += 8) {
                             uint4 w;
@@ -666,16 +688,26 @@ constexpr int kPrepRows = 8 * 256 / D;
 struct PrepMix { uint32_t period, spread, clear_is_rare; };
 constexpr int64_t kPrepManyWarps = 24576;
 // HELD: out from a checkpoint, its integers and exponents.  A lane's eight values lie in one run, so its sum is scaled once;
-// by a power of two, so that it is bit for bit the sum over the values read back.
+// by a power of two, so that it is bit for bit the sum over the values read back.  The CTAs that clear also restore q, k and v:
+// those behind the first n_clear_ctas of them.
+struct RestoreArgs {
+    CkptTensor t[3];
+    uint32_t n_clear_ctas;
+};
 template <int D, bool HELD>
 __global__ void k_bwd_prep(const void* __restrict__ out_, const uint8_t* __restrict__ out_exp, const __nv_bfloat16* __restrict__ dout,
                            const float* __restrict__ lse, int64_t T, int64_t Tpad, int hq, float* __restrict__ dvec,
-                           float* __restrict__ lse2, float4* __restrict__ clear, int64_t n_clear, PrepMix mix, int rounds) {
+                           float* __restrict__ lse2, float4* __restrict__ clear, int64_t n_clear, PrepMix mix, int rounds,
+                           const __grid_constant__ RestoreArgs restore) {
     grid_dep_wait();
     grid_dep_launch();
     const uint32_t turn = blockIdx.x / mix.period, odd = blockIdx.x < mix.spread && blockIdx.x % mix.period == 0;
     const uint32_t rare = blockIdx.x < mix.spread ? turn : mix.spread / mix.period, usual = blockIdx.x - rare - (blockIdx.x < mix.spread);
     if (odd == mix.clear_is_rare) {
+        if (HELD && (odd ? rare : usual) >= restore.n_clear_ctas) {
+            unpack_share(restore.t, ((odd ? rare : usual) - restore.n_clear_ctas) * 8 + (threadIdx.x >> 5));
+            return;
+        }
         int64_t i = (int64_t)(odd ? rare : usual) * (256 * kClearPerThread) + threadIdx.x;
 #pragma unroll
         for (int k = 0; k < kClearPerThread; ++k, i += 256)
@@ -746,16 +778,64 @@ __global__ void k_bwd_prep(const void* __restrict__ out_, const uint8_t* __restr
     }
 }
 
+// Adds up the partial sums of key blocks with tails (dkdv kernel with TAILS), main tile first, then the chunks in order.  Block x: the
+// tail unit of that number, at work where that is the first tail of its key block; the others are `width` apart.  A thread has
+// four columns of a key; few blocks are at work, so the loads of a sum are issued eight at a time (65536 tokens in one sample, 32 / 4
+// heads, 65 sums of 63 terms: 193 us with each address from the term before, 17 now).
+struct TailArgs {
+    const float* partial;
+    const int4* units;
+    const int2* blk;
+    int64_t n_main, T;
+    int n_tails, width, rows;   // rows: row blocks per chunk
+    int hkv;
+    float scale;
+    __nv_bfloat16 *dk, *dv;
+    const int* plan_status;
+};
+constexpr int kSumSplit = 8;        // blocks for a key block's 128 keys
+template <int D>
+__global__ void __launch_bounds__(16 * D / 4) k_sum_tails(const TailArgs a) {
+    grid_dep_wait();
+    if (*a.plan_status != 0) return;
+    const int idx = blockIdx.x, kvh = blockIdx.y >> 1, which = blockIdx.y & 1;
+    const int4 first = a.units[a.n_main + idx];
+    if (first.z == 0 || a.units[first.x].w != idx) return;
+    const int n = (a.blk[first.x].y - 1) / kBlk / a.rows - idx / a.width + 1;   // chunks up to the last that sees the block
+    const int r = blockIdx.z * (kBlk / kSumSplit) + threadIdx.x / (D / 4), col = threadIdx.x % (D / 4) * 4;
+    const size_t slot = (size_t)a.hkv * 2 * kBlk * D;
+    const float* p = a.partial + (((size_t)kvh * 2 + which) * kBlk + r) * D + col;
+    float4 sum = *reinterpret_cast<const float4*>(p + idx * slot);
+    p += (size_t)(a.n_tails + idx) * slot;
+    for (int i = 0; i < n; i += 8) {
+        float4 v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            v[k] = i + k < n ? *reinterpret_cast<const float4*>(p + (size_t)(i + k) * a.width * slot) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) { sum.x += v[k].x; sum.y += v[k].y; sum.z += v[k].z; sum.w += v[k].w; }
+    }
+    const int64_t key = (int64_t)first.x * kBlk + r;
+    if (key >= a.T) return;
+    const float mul = which == 0 ? a.scale : 1.0f;
+    uint2 w;
+    w.x = pack_bf16x2(sum.x * mul, sum.y * mul);
+    w.y = pack_bf16x2(sum.z * mul, sum.w * mul);
+    *reinterpret_cast<uint2*>((which == 0 ? a.dk : a.dv) + ((size_t)key * a.hkv + kvh) * D + col) = w;
+}
+
 struct BwdWorkspace {
     size_t stat_bytes, total;
     size_t dq_acc_bytes, dkv_acc_bytes;   // fused form only: fp32 accumulators of dQ and of dK, dV (each)
+    size_t tail_bytes;                    // two-kernel form with sinks: partial sums of dK and dV
     int64_t Tpad;
 };
-static BwdWorkspace bwd_workspace(int64_t T, int hq, int hkv = 0, int d = 0, bool fused = false) {
+static BwdWorkspace bwd_workspace(int64_t T, int hq, int hkv, int d, bool fused, int n_tails) {
     BwdWorkspace w;
+    w.tail_bytes = fused || d == 256 ? 0 : (size_t)2 * n_tails * hkv * 2 * 128 * d * sizeof(float);
     w.Tpad = (T + 127) / 128 * 128;
     w.stat_bytes = ((size_t)hq * w.Tpad * sizeof(float) + 255) & ~(size_t)255;
-    w.total = 2 * w.stat_bytes;
+    w.total = 2 * w.stat_bytes + w.tail_bytes;
     w.dq_acc_bytes = w.dkv_acc_bytes = 0;
     if (fused) {
         if (d == 128) w.dq_acc_bytes = ((size_t)T * hq * d * sizeof(float) + 255) & ~(size_t)255;
@@ -779,15 +859,17 @@ static int set_smem(Kernel k, int bytes) {
 template <int D>
 static int launch_bwd(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tdo,
                       const CUtensorMap& tdq,
-                      const DkvParams& pa, int Wa, int share, const DqParams& pb, int Wb, libra_plan_t* mp, cudaStream_t s) {
+                      const DkvTailParams& pa, int Wa, int share, const DqSinkParams& pb, int Wb, libra_plan_t* mp, cudaStream_t s) {
     constexpr int kSlot = D == 128 ? 2 : 3;
     if (!cfg_done(kSlot)) {   // per device
-        if (set_smem(k_attn_bwd_dkdv<D, false>, DkvSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
-        if (set_smem(k_attn_bwd_dkdv<D, true>, DkvSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
+        if (set_smem(k_attn_bwd_dkdv<D, false, false>, DkvSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
+        if (set_smem(k_attn_bwd_dkdv<D, true, false>, DkvSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
+        if (set_smem(k_attn_bwd_dkdv<D, false, true>, DkvSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
         if (set_smem(k_attn_bwd_dq<D, false>, DqSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
         if (set_smem(k_attn_bwd_dq<D, true>, DqSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
-        if (!regs_pool_ok(k_attn_bwd_dkdv<D, false>, 128, kDkvRegsDs, 128, kDkvRegsOther)) return LIBRA_ERR_UNSUPPORTED;
-        if (!regs_pool_ok(k_attn_bwd_dkdv<D, true>, 128, kDkvRegsDs, 128, kDkvRegsOther)) return LIBRA_ERR_UNSUPPORTED;
+        if (!regs_pool_ok(k_attn_bwd_dkdv<D, false, false>, 128, kDkvRegsDs, 128, kDkvRegsOther)) return LIBRA_ERR_UNSUPPORTED;
+        if (!regs_pool_ok(k_attn_bwd_dkdv<D, true, false>, 128, kDkvRegsDs, 128, kDkvRegsOther)) return LIBRA_ERR_UNSUPPORTED;
+        if (!regs_pool_ok(k_attn_bwd_dkdv<D, false, true>, 128, kDkvRegsDs, 128, kDkvRegsOther)) return LIBRA_ERR_UNSUPPORTED;
         if (!regs_pool_ok(k_attn_bwd_dq<D, false>, 128 * kDqGroups, kDqRegsCompute, 128, kDqRegsOther)) return LIBRA_ERR_UNSUPPORTED;
         if (!regs_pool_ok(k_attn_bwd_dq<D, true>, 128 * kDqGroups, kDqRegsCompute, 128, kDqRegsOther)) return LIBRA_ERR_UNSUPPORTED;
         cfg_mark(kSlot);
@@ -799,30 +881,51 @@ static int launch_bwd(const CUtensorMap& tq, const CUtensorMap& tk, const CUtens
     mp->n_outcome[1] = (int)grid;
     mp->n_outcome[3] = Wb;
     switch (share) {
-        case 8: e = launch_dependent<8>(k_attn_bwd_dkdv<D, true>, grid, kBwdThreads, bytes, s, tq, tk, tv, tdo, pa); break;
-        case 4: e = launch_dependent<4>(k_attn_bwd_dkdv<D, true>, grid, kBwdThreads, bytes, s, tq, tk, tv, tdo, pa); break;
-        case 2: e = launch_dependent<2>(k_attn_bwd_dkdv<D, true>, grid, kBwdThreads, bytes, s, tq, tk, tv, tdo, pa); break;
-        default: e = launch_dependent(k_attn_bwd_dkdv<D, false>, grid, kBwdThreads, bytes, s, tq, tk, tv, tdo, pa);
+        case 8: e = launch_dependent<8>(k_attn_bwd_dkdv<D, true, false>, grid, kBwdThreads, bytes, s, tq, tk, tv, tdo, pa); break;
+        case 4: e = launch_dependent<4>(k_attn_bwd_dkdv<D, true, false>, grid, kBwdThreads, bytes, s, tq, tk, tv, tdo, pa); break;
+        case 2: e = launch_dependent<2>(k_attn_bwd_dkdv<D, true, false>, grid, kBwdThreads, bytes, s, tq, tk, tv, tdo, pa); break;
+        default:
+            if (pa.units) e = launch_dependent(k_attn_bwd_dkdv<D, false, true>, grid, kBwdThreads, bytes, s, tq, tk, tv, tdo, pa);
+            else e = launch_dependent(k_attn_bwd_dkdv<D, false, false>, grid, kBwdThreads, bytes, s, tq, tk, tv, tdo, pa);
     }
     time_end(mp, 1, s);
     time_begin(mp, 2, s);
     if (e == cudaSuccess)
-        e = launch_dependent(mp->sinks ? k_attn_bwd_dq<D, true> : k_attn_bwd_dq<D, false>, Wb, kDqThreads, DqSmem<D>::kBytes, s, tq, tk,
-                             tv, tdo, tdq, pb);
+        e = mp->sinks ? launch_dependent(k_attn_bwd_dq<D, true>, Wb, kDqThreads, DqSmem<D>::kBytes, s, tq, tk, tv, tdo, tdq, pb)
+                      : launch_dependent(k_attn_bwd_dq<D, false>, Wb, kDqThreads, DqSmem<D>::kBytes, s, tq, tk, tv, tdo, tdq, pb);
     time_end(mp, 2, s);
     count_launch(2);
+    if (pa.units && e == cudaSuccess) {
+        const PlanDir& d = mp->dir[5];
+        time_begin(mp, 5, s);
+        const TailArgs ta = {pa.partial, pa.units, pa.blk, d.NB - d.n_tails, pa.T, d.n_tails, d.tail_width, d.tail_rows, pa.hkv,
+                             pa.scale, pa.dk, pa.dv, pa.plan_status};
+        e = launch_dependent(k_sum_tails<D>, dim3(d.n_tails, 2 * pa.hkv, kSumSplit), 16 * D / 4, 0, s, ta);
+        time_end(mp, 5, s);
+        count_launch();
+    }
     return e == cudaSuccess ? LIBRA_OK : LIBRA_ERR_CUDA;
 }
 
 // Row statistics; `clear` (16-byte words) is zeroed on the way: one pass over memory less to launch.
-struct RowsOut { const void* bf16; const libra_ckpt8* held; };   // one of the two
+struct RowsOut {   // one of the two; `restore`: q, k and v of the checkpoint and where they go
+    const void* bf16;
+    const libra_ckpt8* held;
+    RestoreArgs restore;
+};
 template <int D>
 static cudaError_t launch_prep(const RowsOut& out, const void* dout, const float* lse, int64_t T, int64_t Tpad, int hq, float* dvec,
                                float* lse2, float* clear, size_t clear_bytes, int sms, cudaStream_t s) {
     const int64_t n_clear = (int64_t)(clear_bytes / 16), runs = Tpad / kPrepRows<D> * hq;
     const int rounds = runs >= 4 * kPrepManyWarps ? 4 : (runs > 2 * 8 * ((int64_t)sms - 1) ? 2 : 1);
     static_assert(128 % (4 * kPrepRows<D>) == 0, "rounds of a warp");
-    const int64_t readers = (Tpad / kPrepRows<D> / rounds * hq + 7) / 8, clearers = (n_clear + 256 * kClearPerThread - 1) / (256 * kClearPerThread);
+    const int64_t readers = (Tpad / kPrepRows<D> / rounds * hq + 7) / 8;
+    int64_t clearers = (n_clear + 256 * kClearPerThread - 1) / (256 * kClearPerThread);
+    RestoreArgs restore = out.restore;
+    if (out.held) {
+        restore.n_clear_ctas = (uint32_t)clearers;
+        clearers += (restore.t[0].chunks + restore.t[1].chunks + restore.t[2].chunks + 7) / 8;
+    }
     const int64_t rare = clearers < readers ? clearers : readers, usual = clearers + readers - rare;
     PrepMix mix;
     mix.clear_is_rare = clearers < readers;
@@ -831,7 +934,8 @@ static cudaError_t launch_prep(const RowsOut& out, const void* dout, const float
     count_launch();
     return launch_dependent(out.held ? k_bwd_prep<D, true> : k_bwd_prep<D, false>, (unsigned)(readers + clearers), 256u, 0, s,
                             out.held ? (const void*)out.held->out : out.bf16, out.held ? (const uint8_t*)out.held->out_exp : nullptr,
-                            (const __nv_bfloat16*)dout, lse, T, Tpad, hq, dvec, lse2, (float4*)clear, n_clear, mix, rounds);
+                            (const __nv_bfloat16*)dout, lse, T, Tpad, hq, dvec, lse2, (float4*)clear, n_clear, mix, rounds,
+                            restore);
 }
 
 }  // namespace libra
@@ -843,7 +947,7 @@ extern "C" size_t libra_attn_pool_bwd_workspace_bytes(const libra_plan_t* plan, 
     if (!plan || !dims || dims->hq <= 0 || dims->hkv <= 0 ||
         (dims->head_dim != 64 && dims->head_dim != 128 && dims->head_dim != 256))
         return 0;
-    return bwd_workspace(plan->T, dims->hq, dims->hkv, dims->head_dim, use_fused(plan, dims)).total;
+    return bwd_workspace(plan->T, dims->hq, dims->hkv, dims->head_dim, use_fused(plan, dims), plan->dir[5].n_tails).total;
 }
 
 // fp32 tensor [T, H, 128] viewed as (128, H, T); box = 32 floats x 1 head x 32 rows, 128-byte swizzle.
@@ -894,7 +998,7 @@ static int launch_fused(const void* q_dev, const void* k_dev, const void* v_dev,
         pp.lse2 = lse2; pp.dvec = dvec;
         pp.cta_offsets = wide.d_cta_offsets; pp.cta_tiles = wide.d_cta_exec;
         pp.u_blk = wide.d_u_blk; pp.u_chunk = wide.d_u_chunk; pp.tok_end = plan->d_tok_end;
-        pp.blk_end = plan->d_blk_end; pp.blk_min = plan->d_blk_min;
+        pp.blk = plan->d_blk;
         pp.T = T; pp.Tpad = ws.Tpad; pp.NU = (int)wide.NB;
         pp.hq = dims->hq; pp.hkv = dims->hkv; pp.R = wide.chunk / kBlk;
         pp.scale_log2 = scale * 1.4426950408889634f;
@@ -923,7 +1027,7 @@ static int launch_fused(const void* q_dev, const void* k_dev, const void* v_dev,
         fp.lse2 = lse2; fp.dvec = dvec;
         fp.cta_offsets = d.d_cta_offsets; fp.cta_tiles = d.d_cta_exec;
         fp.u_blk = d.d_u_blk; fp.u_chunk = d.d_u_chunk; fp.tok_end = plan->d_tok_end;
-        fp.blk_end = plan->d_blk_end; fp.blk_min = plan->d_blk_min;
+        fp.blk = plan->d_blk;
         fp.T = T; fp.Tpad = ws.Tpad; fp.NU = d.NB;
         fp.hq = dims->hq; fp.hkv = dims->hkv; fp.R = d.chunk / d.tile;
         fp.scale_log2 = scale * 1.4426950408889634f;
@@ -960,7 +1064,7 @@ static RestoredQkv restored_qkv(size_t own, const libra_dims* dims) {
 }
 
 // held: q, k, v and out come from a checkpoint, q_dev, k_dev and v_dev are null.
-static int backward(const void* q_dev, const void* k_dev, const void* v_dev, const RowsOut& out, const float* lse_dev,
+static int backward(const void* q_dev, const void* k_dev, const void* v_dev, RowsOut out, const float* lse_dev,
                     const void* dout_dev, const libra_plan_t* plan, void* dq_dev, void* dk_dev, void* dv_dev, void* workspace_dev,
                     const libra_dims* dims, void* stream) {
     if (dims->hq <= 0 || dims->hkv <= 0 || dims->hq % dims->hkv) return LIBRA_ERR_INVALID_ARG;
@@ -992,7 +1096,7 @@ static int backward(const void* q_dev, const void* k_dev, const void* v_dev, con
 
     const int D = dims->head_dim;
     const int64_t T = plan->T;
-    const BwdWorkspace ws = bwd_workspace(T, dims->hq, dims->hkv, D, fused);
+    const BwdWorkspace ws = bwd_workspace(T, dims->hq, dims->hkv, D, fused, plan->dir[5].n_tails);
     float* dvec = reinterpret_cast<float*>(workspace_dev);
     float* lse2 = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace_dev) + ws.stat_bytes);
     cudaStream_t s = (cudaStream_t)stream;
@@ -1002,15 +1106,14 @@ static int backward(const void* q_dev, const void* k_dev, const void* v_dev, con
     if (out.held) {
         const RestoredQkv r = restored_qkv(ws.total, dims);
         uint8_t* w = reinterpret_cast<uint8_t*>(workspace_dev);
-        time_begin(const_cast<libra_plan_t*>(plan), 3, s);
-        if (const int rc = launch_ckpt8_restore(out.held, w + r.q, w + r.k, w + r.v, dims, plan->d_status, s); rc != LIBRA_OK) return rc;
         q_dev = w + r.q;
         k_dev = w + r.k;
         v_dev = w + r.v;
+        if (!set_restore(out.restore.t, out.held, w + r.q, w + r.k, w + r.v, dims)) return LIBRA_ERR_INVALID_ARG;
     }
     if (D == 256) {   // row statistics, then the three passes of the 256-wide kernel
         libra_plan_t* mp256 = const_cast<libra_plan_t*>(plan);
-        if (!out.held) time_begin(mp256, 3, s);
+        time_begin(mp256, 3, s);
         float* dk_acc = nullptr;
         float* dv_acc = nullptr;
         if (fused) {
@@ -1042,7 +1145,7 @@ static int backward(const void* q_dev, const void* k_dev, const void* v_dev, con
     if (rc != LIBRA_OK) return rc;
 
     libra_plan_t* mp0 = const_cast<libra_plan_t*>(plan);
-    if (!out.held) time_begin(mp0, 3, s);
+    time_begin(mp0, 3, s);
     {
         float* acc = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace_dev) + 2 * ws.stat_bytes);
         const size_t acc_bytes = fused ? ws.dq_acc_bytes + 2 * ws.dkv_acc_bytes : 0;   // the three accumulators are contiguous
@@ -1055,16 +1158,18 @@ static int backward(const void* q_dev, const void* k_dev, const void* v_dev, con
     if (fused)
         return launch_fused(q_dev, k_dev, v_dev, dout_dev, dq_dev, dk_dev, dv_dev, reinterpret_cast<uint8_t*>(workspace_dev),
                             ws, plan, dims, scale, s);
-    DkvParams pa;
+    DkvTailParams pa;
     pa.dk = reinterpret_cast<__nv_bfloat16*>(dk_dev);
     pa.dv = reinterpret_cast<__nv_bfloat16*>(dv_dev);
     pa.lse2 = lse2;
     pa.dvec = dvec;
-    pa.cta_offsets = dkv_dir.d_cta_offsets;
-    pa.cta_tiles = dkv_dir.d_cta_exec;
+    const PlanDir& dkv_lists = plan->sinks ? plan->dir[5] : dkv_dir;
+    pa.cta_offsets = dkv_lists.d_cta_offsets;
+    pa.cta_tiles = dkv_lists.d_cta_exec;
+    pa.units = dkv_lists.d_units;
+    pa.partial = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace_dev) + 2 * ws.stat_bytes);
     pa.tok_end = plan->d_tok_end;
-    pa.blk_end = plan->d_blk_end;
-    pa.blk_min = plan->d_blk_min;
+    pa.blk = plan->d_blk;
     pa.T = T;
     pa.Tpad = ws.Tpad;
     pa.hq = dims->hq;
@@ -1076,7 +1181,7 @@ static int backward(const void* q_dev, const void* k_dev, const void* v_dev, con
     pa.wait_limit_ns = plan->wait_limit_ns;
     pa.inject_stall = plan->inject_stall;
     pa.busy = dkv_dir.d_busy;
-    DqParams pb;
+    DqSinkParams pb;
     pb.dq = reinterpret_cast<__nv_bfloat16*>(dq_dev);
     pb.lse2 = lse2;
     pb.dvec = dvec;
@@ -1104,7 +1209,7 @@ static int backward(const void* q_dev, const void* k_dev, const void* v_dev, con
     int64_t reach = T / plan->n;   // rows that see a key block, on average
     if (plan->window && reach > plan->window + kBlk) reach = plan->window + kBlk;
     const int64_t its = (int64_t)(dims->hq / dims->hkv) * reach / kBlk;
-    int share = dims->hq > dims->hkv ? 8 : 1;
+    int share = dims->hq > dims->hkv && !pa.units ? 8 : 1;
     while (share > 1 && (share * dkv_dir.NT > dkv_dir.W || 2 * share > its)) share /= 2;
     libra_plan_t* mp = const_cast<libra_plan_t*>(plan);
     return D == 128 ? launch_bwd<128>(tq, tk, tv, tdo, tdq, pa, dkv_dir.W, share, pb, dq_dir.W, mp, s)
@@ -1118,7 +1223,7 @@ extern "C" int libra_attn_pool_bwd(const void* q_dev, const void* k_dev, const v
     if (!q_dev || !k_dev || !v_dev || !out_dev || !lse_dev || !dout_dev || !cu_seqlens_dev || !plan || !dq_dev ||
         !dk_dev || !dv_dev || !workspace_dev || !dims)
         return LIBRA_ERR_INVALID_ARG;
-    return backward(q_dev, k_dev, v_dev, {out_dev, nullptr}, lse_dev, dout_dev, plan, dq_dev, dk_dev, dv_dev, workspace_dev, dims, stream);
+    return backward(q_dev, k_dev, v_dev, {out_dev, nullptr, {}}, lse_dev, dout_dev, plan, dq_dev, dk_dev, dv_dev, workspace_dev, dims, stream);
 }
 
 extern "C" size_t libra_attn_pool_bwd_ckpt8_workspace_bytes(const libra_plan_t* plan, const libra_dims* dims) {
@@ -1133,5 +1238,5 @@ extern "C" int libra_attn_pool_bwd_ckpt8(const libra_ckpt8* ckpt, const float* l
         return LIBRA_ERR_INVALID_ARG;
     if (!ckpt->q || !ckpt->k || !ckpt->v || !ckpt->out || !ckpt->q_exp || !ckpt->k_exp || !ckpt->v_exp || !ckpt->out_exp)
         return LIBRA_ERR_INVALID_ARG;
-    return backward(nullptr, nullptr, nullptr, {nullptr, ckpt}, lse_dev, dout_dev, plan, dq_dev, dk_dev, dv_dev, workspace_dev, dims, stream);
+    return backward(nullptr, nullptr, nullptr, {nullptr, ckpt, {}}, lse_dev, dout_dev, plan, dq_dev, dk_dev, dv_dev, workspace_dev, dims, stream);
 }

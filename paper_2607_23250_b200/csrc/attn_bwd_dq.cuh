@@ -52,10 +52,8 @@ struct DqParams {
     const int32_t* cta_offsets;
     const int32_t* cta_tiles;
     const int32_t* tok_start;
-    const int32_t* tok_first;   // SINK: first token of the row's sample
     int64_t T, Tpad;
     int hq, hkv, H;
-    int sinks;
     float scale, scale_log2;
     int* outcome;
     int side_by_side;        // start without waiting for the dK/dV kernel
@@ -65,24 +63,56 @@ struct DqParams {
     uint64_t* busy;
 };
 
+struct DqSinkParams : DqParams {   // (of the instance with sinks: longer arguments cost the other one registers)
+    const int32_t* tok_first;      // first token of the row's sample
+    int sinks;
+};
+
 // Walks the units of one CTA in the order every role uses: tiles of the CTA's list x the two 128-row
 // sub-blocks of a tile x the heads of the shard.  A sub-block past the end of the pool is skipped.
 template <bool SINK>
-struct DqUnit {
+struct DqUnitSinks {};
+template <>
+struct DqUnitSinks<true> {
+    int slo, shi;   // blocks ahead of the others, slo..shi < lo, which hold the sinks of the first row's sample,
+    int sfirst;     // from this one on
+};
+template <bool SINK>
+struct DqUnit : DqUnitSinks<SINK> {
     int64_t q0;
     int lo, hi, h;  // key blocks lo..hi, query head h
-    int slo, shi;   // SINK: and, ahead of them, slo..shi < lo, which hold the sinks of the first row's sample
     bool valid;
-    __device__ __forceinline__ int first() const { return SINK && slo <= shi ? slo : lo; }
-    __device__ __forceinline__ int after(int j) const { return SINK && j == shi ? lo : j + 1; }
-    __device__ __forceinline__ int count() const { return hi - lo + 1 + (SINK && slo <= shi ? shi - slo + 1 : 0); }
+    __device__ __forceinline__ int first() const {
+        if constexpr (SINK) { if (this->slo <= this->shi) return this->slo; }
+        return lo;
+    }
+    __device__ __forceinline__ int after(int j) const {
+        if constexpr (SINK) { if (j == this->shi) return lo; }
+        return j + 1;
+    }
+    __device__ __forceinline__ int count() const {
+        if constexpr (SINK) { if (this->slo <= this->shi) return hi - lo + 1 + this->shi - this->slo + 1; }
+        return hi - lo + 1;
+    }
+    // Of a block ahead of the window only the 32-column groups that hold one of the n sinks are computed: c0 .. c1.
+    __device__ __forceinline__ void sink_groups(int j, int n, int& c0, int& c1) const {
+        c0 = 0;
+        c1 = kBlk / 32 - 1;
+        if constexpr (SINK) {
+            if (j >= lo) return;
+            const int64_t a = this->sfirst - (int64_t)j * kBlk, z = a + n - 1;
+            c0 = a > 0 ? (int)a / 32 : 0;
+            c1 = z < kBlk - 1 ? (int)z / 32 : c1;
+        }
+    }
 };
 template <bool SINK>
 struct DqUnitIter {
-    const DqParams& p;
+    using P = std::conditional_t<SINK, DqSinkParams, DqParams>;
+    const P& p;
     int idx, end, sub, hh, hps;
     int t;  // cta_tiles[idx], fetched when idx moves so that the load has a unit's time to land
-    __device__ DqUnitIter(const DqParams& p_, int begin, int end_, int heads_per_shard)
+    __device__ DqUnitIter(const P& p_, int begin, int end_, int heads_per_shard)
         : p(p_), idx(begin), end(end_), sub(0), hh(0), hps(heads_per_shard) {
         t = idx < end ? p.cta_tiles[idx] : 0;
     }
@@ -96,10 +126,11 @@ struct DqUnitIter {
                 u.q0 = q0;
                 u.lo = p.tok_start[q0] / kBlk;
                 u.hi = (int)(q0 / kBlk);
-                if (SINK) {
+                if constexpr (SINK) {
                     const int first = p.tok_first[q0];
                     const int64_t end = (int64_t)first + p.sinks;
                     u.slo = first / kBlk;
+                    u.sfirst = first;
                     u.shi = min((int)((end < p.T ? end : p.T) - 1) / kBlk, u.lo - 1);
                     if (u.shi < u.slo) u.shi = -1;
                 }
@@ -124,8 +155,10 @@ template <int D, bool SINK>
 __global__ void __launch_bounds__(kDqThreads, 1)
 k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
               const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_do,
-              const __grid_constant__ CUtensorMap tm_dq, const DqParams p) {
+              const __grid_constant__ CUtensorMap tm_dq, const typename DqUnitIter<SINK>::P p) {
     using L = DqSmem<D>;
+    int n_sinks = 0;
+    if constexpr (SINK) n_sinks = p.sinks;
     extern __shared__ __align__(1024) uint8_t smem[];
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBarOff);
     uint64_t* bar_qfull = bars + 0;
@@ -338,8 +371,18 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             const uint64_t mdesc0 = make_sdesc(sb, L::kHalfBytes, 1024);  // MN-major view
             uint32_t kcnt = 0, vcnt = 0, blk = 0;
             bool ok = true;
-            // C[tmem d_col] = A[tmem a_col, bf16 packed over the head dimension] * B(K-major tile at b_off)^T
-            auto issue_qk = [&](uint32_t d_col, uint32_t a_col, uint32_t b_off) {
+            // C[tmem d_col] = A[tmem a_col, bf16 packed over the head dimension] * B(K-major tile at b_off)^T, the columns of the
+            // groups c0 .. c1 (SINK; otherwise all)
+            auto issue_qk = [&](uint32_t d_col, uint32_t a_col, uint32_t b_off, int c0, int c1) {
+                if (SINK && c1 - c0 != kBlk / 32 - 1) {
+                    const uint64_t db = sdesc_advance(kdesc0, b_off + c0 * 4096);   // 32 rows of 128 bytes a group
+                    const uint32_t idesc = make_idesc(128, 32 * (c1 - c0 + 1), 0, 0);
+#pragma unroll 1
+                    for (int kk = 0; kk < D / 16; ++kk)
+                        mma_ts(tmem_base + d_col + 32 * c0, tmem_base + a_col + kk * 8,
+                               sdesc_advance(db, (kk / 4) * L::kHalfBytes + (kk % 4) * 32), idesc, kk > 0);
+                    return;
+                }
                 const uint64_t db = sdesc_advance(kdesc0, b_off);
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk) {
@@ -347,20 +390,24 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                     mma_ts(tmem_base + d_col, tmem_base + a_col + kk * 8, sdesc_advance(db, off), idesc_s, kk > 0);
                 }
             };
-            // S(j) from K ring entry kidx
-            auto do_s = [&](uint32_t kidx) -> bool {
+            // S(j) of unit un from K ring entry kidx
+            auto do_s = [&](uint32_t kidx, const DqUnit<SINK>& un, int j) -> bool {
                 if (!mbar_wait(&bar_kfull[kidx % L::kKStages], (kidx / L::kKStages) & 1, abort_flag)) return false;
                 {
-                    issue_qk(kColS, kColQ, L::kKOff + (kidx % L::kKStages) * L::kTileBytes);
+                    int c0, c1;
+                    un.sink_groups(j, n_sinks, c0, c1);
+                    issue_qk(kColS, kColQ, L::kKOff + (kidx % L::kKStages) * L::kTileBytes, c0, c1);
                     tc_commit(bar_sfull);
                 }
                 return true;
             };
-            auto do_dp = [&]() -> bool {
+            auto do_dp = [&](const DqUnit<SINK>& un, int j) -> bool {
                 const uint32_t vs = vcnt % L::kVStages;
                 if (!mbar_wait(&bar_vfull[vs], (vcnt / L::kVStages) & 1, abort_flag)) return false;
                 {
-                    issue_qk(kColDP, kColDO, L::kVOff + vs * L::kTileBytes);
+                    int c0, c1;
+                    un.sink_groups(j, n_sinks, c0, c1);
+                    issue_qk(kColDP, kColDO, L::kVOff + vs * L::kTileBytes, c0, c1);
                     tc_commit(bar_dpfull);
                     tc_commit(&bar_vempty[vs]);
                 }
@@ -372,22 +419,23 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             uint32_t ucnt = 0;
             if (u.valid) {  // first unit: nothing to overlap its first S and dP with
                 ok = mbar_wait(bar_qtready, 0, abort_flag);
-                if (ok) { tc_fence_after(); ok = do_s(kcnt); }
+                if (ok) { tc_fence_after(); ok = do_s(kcnt, u, u.first()); }
                 if (ok) ok = mbar_wait(bar_dotready, 0, abort_flag);
-                if (ok) { tc_fence_after(); ok = do_dp(); }
+                if (ok) { tc_fence_after(); ok = do_dp(u, u.first()); }
             }
             while (u.valid && ok) {
                 const DqUnit<SINK> nx = units.next();
                 const int n = u.count();
                 const uint32_t kbase = kcnt;  // ring index of the first block's K
-                for (int i = 0; i < n && ok; ++i, ++blk) {
+                for (int i = 0, j = u.first(), jn; i < n && ok; ++i, ++blk, j = jn) {
                     const bool last = i == n - 1;
+                    jn = u.after(j);
                     // S(j+1) as soon as the compute groups have read S(j)
                     if (!last) {
                         ok = mbar_wait(bar_sfree, blk & 1, abort_flag);
                         if (!ok) break;
                         tc_fence_after();
-                        ok = do_s(kbase + i + 1);
+                        ok = do_s(kbase + i + 1, u, jn);
                         if (!ok) break;
                     }
                     // dQ += dS(j) K_j
@@ -398,16 +446,26 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                     const uint32_t kidx = kbase + i;
                     {
                         const uint64_t ka = sdesc_advance(mdesc0, L::kKOff + (kidx % L::kKStages) * L::kTileBytes);
+                        int c0, c1;
+                        u.sink_groups(j, n_sinks, c0, c1);
+                        if (SINK && c1 - c0 != kBlk / 32 - 1) {
+#pragma unroll 1
+                            for (int kk = 2 * c0; kk <= 2 * c1 + 1; ++kk)
+                                mma_ts(tmem_base + kColDQ,
+                                       tmem_base + kColDP + (kk / (kDqCW / 16)) * kDqCW + (kk % (kDqCW / 16)) * 8,
+                                       sdesc_advance(ka, kk * 2048), idesc_dq, (i > 0 || kk > 2 * c0) ? 1u : 0u);
+                        } else {
 #pragma unroll
                         for (int kk = 0; kk < 8; ++kk)  // 16 keys per step; group c left dS of its keys at columns CW c ..
                             mma_ts(tmem_base + kColDQ,
                                    tmem_base + kColDP + (kk / (kDqCW / 16)) * kDqCW + (kk % (kDqCW / 16)) * 8,
                                    sdesc_advance(ka, kk * 2048), idesc_dq, (i > 0 || kk > 0) ? 1u : 0u);
+                        }
                         tc_commit(&bar_kempty[kidx % L::kKStages]);
                         if (last) tc_commit(bar_dqfull);
                     }
                     if (!last) {
-                        ok = do_dp();  // dP(j+1) over dS(j), after dQ(j) in pipe order
+                        ok = do_dp(u, jn);  // dP(j+1) over dS(j), after dQ(j) in pipe order
                     } else if (nx.valid) {
                         // first block of the next unit, behind the last dQ of this one: its Q and dO rows
                         // were copied into TMEM while that dQ ran
@@ -415,11 +473,11 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                         if (ok) ok = mbar_wait(bar_qtready, (ucnt + 1) & 1, abort_flag);
                         if (!ok) break;
                         tc_fence_after();
-                        ok = do_s(kbase + n);
+                        ok = do_s(kbase + n, nx, nx.first());
                         if (ok) ok = mbar_wait(bar_dotready, (ucnt + 1) & 1, abort_flag);
                         if (!ok) break;
                         tc_fence_after();
-                        ok = do_dp();
+                        ok = do_dp(nx, nx.first());
                     }
                 }
                 kcnt = kbase + n;
@@ -482,9 +540,11 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             x.max_kstart = p.tok_start[last_row];
             x.sink_lo = 0;
             x.sink_hi = -1;
-            if (SINK && x.row_ok) {
-                x.sink_lo = p.tok_first[row];
-                x.sink_hi = (int)min((int64_t)x.sink_lo + p.sinks, (int64_t)x.kstart) - 1;
+            if constexpr (SINK) {
+                if (x.row_ok) {
+                    x.sink_lo = p.tok_first[row];
+                    x.sink_hi = (int)min((int64_t)x.sink_lo + n_sinks, (int64_t)x.kstart) - 1;
+                }
             }
             x.lse2 = p.lse2[(size_t)un.h * p.Tpad + row];  // padded rows hold zeros
             x.dsum = p.dvec[(size_t)un.h * p.Tpad + row];
@@ -516,6 +576,16 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                 ok = warp_wait(bar_sfull, blk & 1, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
+                int g0, g1;
+                u.sink_groups(j, n_sinks, g0, g1);
+                static_assert(!SINK || CW == 32, "a group of columns per compute group");
+                if (SINK && (c < g0 || c > g1)) {   // nothing of this group's columns is computed (nor the unit's last block)
+                    mbar_arrive(bar_sfree);
+                    ok = warp_wait(bar_dpfull, blk & 1, abort_flag);
+                    if (!ok) break;
+                    mbar_arrive(bar_dsready);
+                    continue;
+                }
                 uint32_t sv[CW];
 #pragma unroll
                 for (int i = 0; i < CW; i += 32) tmem_ld32(t_s + i, sv + i);

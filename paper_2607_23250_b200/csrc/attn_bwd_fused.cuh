@@ -63,8 +63,7 @@ struct FusedParams {
     const int32_t* u_blk;     // key block of pair-block u
     const int32_t* u_chunk;   // query chunk of pair-block u
     const int32_t* tok_end;
-    const int32_t* blk_end;   // of the block's keys the largest tok_end, and a bound from below
-    const int32_t* blk_min;
+    const int2* blk;          // of the block's keys at most the smallest tok_end, and the largest
     int64_t T, Tpad, NU;
     int hq, hkv, R;           // R = row blocks per query chunk
     float scale_log2;
@@ -87,7 +86,7 @@ __device__ __forceinline__ FusedUnit fused_unit(const FusedParams& p, int t) {
     u.kvh = (int)(t / p.NU);
     const int j = p.u_blk[pb], c = p.u_chunk[pb];
     u.k0 = (int64_t)j * kBlk;
-    const int last = last_q_block(p.blk_end, u.k0);
+    const int last = last_q_block(p.blk, u.k0);
     const int lo = c * p.R > j ? c * p.R : j;
     const int hi = c * p.R + p.R - 1 < last ? c * p.R + p.R - 1 : last;
     u.i0 = lo;
@@ -519,7 +518,7 @@ k_attn_bwd_fused(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             const int64_t key = u.k0 + r;
             const bool key_ok = key < p.T;
             const int kend = key_ok ? p.tok_end[key] : 0;
-            const int min_kend = p.blk_min[u.k0 / kBlk];
+            const int min_kend = p.blk[u.k0 / kBlk].x;
             const bool partial = u.k0 + kBlk > p.T;
             for (int it = 0, i = 0; it < n_it && ok; ++it, ++it_all) {
                 const int qb = (u.i0 + i) * kBlk;

@@ -90,8 +90,7 @@ struct PairParams {
     const int32_t* u_blk;     // 256-key block of wide pair-block u
     const int32_t* u_chunk;   // query chunk of it
     const int32_t* tok_end;
-    const int32_t* blk_end;   // of a 128-key block's keys the largest tok_end, and a bound from below
-    const int32_t* blk_min;
+    const int2* blk;          // of a 128-key block's keys at most the smallest tok_end, and the largest
     int64_t T, Tpad;
     int NU;                   // wide pair-blocks
     int hq, hkv, R;           // R = row blocks per query chunk
@@ -137,9 +136,9 @@ __device__ __forceinline__ PairUnit pair_unit(const PairParams& p, int t) {
     u.j0 = 2 * p.u_blk[pb];
     u.c = p.u_chunk[pb];
     const int64_t k1 = (int64_t)(u.j0 + 1) * kBlk;
-    u.last0 = last_q_block(p.blk_end, (int64_t)u.j0 * kBlk);
+    u.last0 = last_q_block(p.blk, (int64_t)u.j0 * kBlk);
     u.two = k1 < p.T;
-    u.last1 = u.two ? last_q_block(p.blk_end, k1) : u.last0;
+    u.last1 = u.two ? last_q_block(p.blk, k1) : u.last0;
     const int last = u.last1 > u.last0 ? u.last1 : u.last0;
     const int lo = u.c * p.R > u.j0 ? u.c * p.R : u.j0;
     const int hi = u.c * p.R + p.R - 1 < last ? u.c * p.R + p.R - 1 : last;
@@ -587,7 +586,7 @@ k_attn_bwd_pair(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             const int64_t k0 = (int64_t)(u.j0 + rank) * kBlk, key = k0 + r;
             const bool key_ok = key < p.T;
             const int kend = key_ok ? p.tok_end[key] : 0;
-            const int min_kend = k0 < p.T ? p.blk_min[k0 / kBlk] : 0;
+            const int min_kend = k0 < p.T ? p.blk[k0 / kBlk].x : 0;
             const bool partial = k0 + kBlk > p.T;
             for (int it = 0, i = 0; it < n_it && ok; ++it, ++n) {
                 const int qb = (u.i0 + i) * kBlk;

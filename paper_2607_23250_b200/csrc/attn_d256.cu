@@ -104,7 +104,7 @@ struct Params {
     const int32_t* cta_tiles;
     const int32_t* tok_start;
     const int32_t* tok_end;
-    const int32_t* blk_end; // [ceil(T / 128)] largest tok_end of a block's keys
+    const int2* blk;        // [ceil(T / 128)] of a block's keys at most the smallest tok_end, and the largest
     const int32_t* tok_first;   // SINK: first token of the row's sample
     int sinks;
     int64_t T, Tpad;
@@ -163,8 +163,8 @@ struct Units {
             const int j = p.acc32 ? p.u_blk[(int)(t % p.NU)] : t / p.hkv;
             kvh = p.acc32 ? (int)(t / p.NU) : t % p.hkv;
             base = (int64_t)j * (2 * kRows);
-            bound0 = p.blk_end[base / kRows];
-            bound1 = base + kRows < p.T ? p.blk_end[base / kRows + 1] : bound0;
+            bound0 = p.blk[base / kRows].y;
+            bound1 = base + kRows < p.T ? p.blk[base / kRows + 1].y : bound0;
             int last64 = ((bound1 > bound0 ? bound1 : bound0) - 1) / kBlk;
             b_lo = (int)(base / kBlk);
             if (p.acc32) {   // pair tile: the query blocks of one chunk only
@@ -866,7 +866,7 @@ int launch_fwd_d256(const void* q, const void* k, const void* v, void* out, floa
     prm.cta_tiles = d.d_cta_exec;
     prm.tok_start = plan->d_tok_start;
     prm.tok_end = plan->d_tok_end;
-    prm.blk_end = plan->d_blk_end;
+    prm.blk = plan->d_blk;
     prm.tok_first = plan->d_tok_first;
     prm.sinks = plan->sinks;
     prm.T = plan->T;
@@ -908,7 +908,7 @@ int launch_bwd_d256(const void* q, const void* k, const void* v, const void* dou
     prm.lse2 = lse2; prm.dvec = dvec;
     prm.tok_start = plan->d_tok_start;
     prm.tok_end = plan->d_tok_end;
-    prm.blk_end = plan->d_blk_end;
+    prm.blk = plan->d_blk;
     prm.tok_first = plan->d_tok_first;
     prm.sinks = plan->sinks;
     prm.T = plan->T;

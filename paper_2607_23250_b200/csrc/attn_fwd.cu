@@ -9,6 +9,7 @@
 // A window moves the first key of a row (tok_start) closer and changes nothing else: it never decreases from row to row, like
 // the start of a sample.  With sinks (SINK) a slot goes through a second run of blocks, those that hold the sinks of its
 // first row's sample and lie ahead of its window, after the others; a masked block's visible columns are then two ranges.
+// Of such a block only the 32-column groups that hold a sink are computed (S, exponentials and PV).
 //
 // Roles (384 threads): warps 0-3 and 4-7 are the softmax groups of slot 0 and 1 (one row per
 // thread, S read from TMEM, P written back to TMEM as bf16 over S), warp 8 issues TMA loads,
@@ -85,19 +86,38 @@ struct FwdParams {
 // SINK: also blocks slo[g] .. shi[g] < lo[g].  What slot 1 sees lies among slot 1's diagonal block and what slot 0 sees: its
 // first row's sample is slot 0's, or starts in slot 0.
 template <bool SINK>
-struct FwdTile {
+struct FwdTileSinks {};
+template <>
+struct FwdTileSinks<true> {
+    int slo[2], shi[2];
+    int first[2];       // first sink that the slot's first row sees
+    // The 32-column groups c0 .. c1 of block j that hold one of its n sinks.
+    __device__ __forceinline__ void sink_groups(int g, int j, int n, int& c0, int& c1) const {
+        const int64_t a = first[g] - (int64_t)j * kBN, z = a + n - 1;
+        c0 = a > 0 ? (int)a / 32 : 0;
+        c1 = z < kBN - 1 ? (int)z / 32 : kBN / 32 - 1;
+    }
+};
+template <bool SINK>
+struct FwdTile : FwdTileSinks<SINK> {
     int t;
     int64_t q0;
     int lo[2], hi[2];
-    int slo[SINK ? 2 : 1], shi[SINK ? 2 : 1];
-    // The walk of the tile, downwards: the block after j, of slot g (0: of the tile), -1 at the end (SINK only).
-    __device__ __forceinline__ int after(int j, int g) const {
-        if (j == (j >= lo[g] ? lo[g] : slo[g])) return j >= lo[g] && shi[g] >= slo[g] ? shi[g] : -1;
+    // The walk of the tile, downwards: the block after j, -1 at the end (only with SINK).
+    __device__ __forceinline__ int after(int j) const {
+        if constexpr (SINK) {
+            if (j == lo[0]) return this->shi[0] >= this->slo[0] ? this->shi[0] : -1;
+            if (j < lo[0] && j == this->slo[0]) return -1;
+        }
         return j - 1;
     }
-    __device__ __forceinline__ int last() const { return SINK && shi[0] >= slo[0] ? slo[0] : lo[0]; }
+    __device__ __forceinline__ int last() const {
+        if constexpr (SINK) return this->shi[0] >= this->slo[0] ? this->slo[0] : lo[0];
+        return lo[0];
+    }
     __device__ __forceinline__ bool sees(int g, int j) const {
-        return (j >= lo[g] && j <= hi[g]) || (SINK && j >= slo[g] && j <= shi[g]);
+        if constexpr (SINK) { if (j >= this->slo[g] && j <= this->shi[g]) return true; }
+        return j >= lo[g] && j <= hi[g];
     }
     // A tile that a pair of CTAs shares: `shared`, and part[g] when both have key blocks of slot g.
     bool shared, part[2];
@@ -120,13 +140,15 @@ struct FwdTile {
 // Walks the list.  Ids are fetched two tiles and sample starts one tile ahead: a chain of two dependent global
 // loads between tiles would leave the tensor pipe idle for about 2000 clk.
 template <bool SINK>
-struct FwdTiles {
+struct FwdTilesSinks {};
+template <>
+struct FwdTilesSinks<true> { int a0 = 0, b0 = 0; };   // tok_first of the first row of each slot
+template <bool SINK>
+struct FwdTiles : FwdTilesSinks<SINK> {
     const FwdParams& p;
     int idx, end;
     int t1, t2, a1, b1;   // next tile: id, tok_start of the first row of each slot; id of the one after
-    int a0, b0;           // SINK: the same rows' tok_first
-    __device__ __forceinline__ FwdTiles(const FwdParams& p_, int begin, int end_)
-        : p(p_), idx(begin), end(end_), a1(0), b1(0), a0(0), b0(0) {
+    __device__ __forceinline__ FwdTiles(const FwdParams& p_, int begin, int end_) : p(p_), idx(begin), end(end_), a1(0), b1(0) {
         t1 = idx < end ? p.cta_tiles[idx] : -1;
         t2 = idx + 1 < end ? p.cta_tiles[idx + 1] : -1;
         fetch();
@@ -136,9 +158,9 @@ struct FwdTiles {
         const int64_t q0 = (int64_t)(t1 / p.H) * (2 * kBM);
         a1 = p.tok_start[q0];
         b1 = q0 + kBM < p.T ? p.tok_start[q0 + kBM] : 0;
-        if (SINK) {
-            a0 = p.tok_first[q0];
-            b0 = q0 + kBM < p.T ? p.tok_first[q0 + kBM] : 0;
+        if constexpr (SINK) {
+            this->a0 = p.tok_first[q0];
+            this->b0 = q0 + kBM < p.T ? p.tok_first[q0 + kBM] : 0;
         }
     }
     // Last block that holds a sink of a sample starting at `first`.
@@ -156,10 +178,12 @@ struct FwdTiles {
         x.hi[1] = two ? x.hi[0] + 1 : -1;
         x.lo[1] = two ? b1 / kBN : 0;
         if constexpr (SINK) {
-            x.slo[0] = a0 / kBN;
-            x.shi[0] = min(sink_block(a0), x.lo[0] - 1);
-            x.slo[1] = two ? b0 / kBN : 0;
-            x.shi[1] = two ? min(sink_block(b0), x.lo[1] - 1) : -1;
+            x.first[0] = this->a0;
+            x.first[1] = this->b0;
+            x.slo[0] = this->a0 / kBN;
+            x.shi[0] = min(sink_block(this->a0), x.lo[0] - 1);
+            x.slo[1] = two ? this->b0 / kBN : 0;
+            x.shi[1] = two ? min(sink_block(this->b0), x.lo[1] - 1) : -1;
         }
         ++idx;
         t1 = t2;
@@ -330,7 +354,7 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
                 for (int hh = 0; hh < heads_per_shard && ok; ++hh) {
                     const int h = (x.t % p.H) * heads_per_shard + hh;
                     const int kvh = h / G;
-                    for (int j = top; (SINK ? j >= 0 : j >= x.lo[0]) && ok; j = SINK ? x.after(j, 0) : j - 1) {
+                    for (int j = top; (SINK ? j >= 0 : j >= x.lo[0]) && ok; j = x.after(j)) {
                         for (int kv = 0; kv < 2; ++kv) {  // K_j then V_j
                             const uint32_t st = ring % L::kStages;
                             ok = mbar_wait(&bar_empty[st], ((ring / L::kStages) & 1) ^ 1, abort_flag);
@@ -387,6 +411,20 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
                 }
                 tc_commit(&bar_sfull[g]);
             };
+            // SINK, a block ahead of the slot's window: the columns of the groups c0 .. c1 alone
+            auto issue_sink_s = [&](const auto& x, int g, uint32_t stage, int j) {
+                int c0, c1;
+                x.sink_groups(g, j, p.sinks, c0, c1);
+                const uint64_t qa = sdesc_advance(desc_q, g * L::kTileBytes);
+                const uint64_t ka = sdesc_advance(desc_k, stage * L::kTileBytes + c0 * 4096);   // 32 rows of 128 bytes a group
+                const uint32_t idesc = make_idesc(kBM, 32 * (c1 - c0 + 1), 0, 0);
+#pragma unroll 1
+                for (int kk = 0; kk < D / 16; ++kk) {
+                    const uint32_t off = (kk / 4) * L::kHalfBytes + (kk % 4) * 32;
+                    mma_ss(tmem_base + g * kBN + 32 * c0, sdesc_advance(qa, off), sdesc_advance(ka, off), idesc, kk > 0);
+                }
+                tc_commit(&bar_sfull[g]);
+            };
             // O[g] (+)= P[g] V over the key steps [kk0, kk1) of 16 keys; the softmax group hands P over in two parts
             auto issue_pv = [&](int g, uint32_t stage, bool accumulate, int kk0, int kk1) {
                 const uint64_t va = sdesc_advance(desc_v, stage * L::kTileBytes);
@@ -396,6 +434,15 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
                            (accumulate || kk > 0) ? 1u : 0u);
                 }
                 if (kk1 == kBN / 16) tc_commit(&bar_odone[g]);
+            };
+            auto issue_sink_pv = [&](const auto& x, int g, uint32_t stage, int j) {
+                int c0, c1;
+                x.sink_groups(g, j, p.sinks, c0, c1);
+                const uint64_t va = sdesc_advance(desc_v, stage * L::kTileBytes);
+#pragma unroll 1
+                for (int kk = 2 * c0; kk <= 2 * c1 + 1; ++kk)
+                    mma_ts(tmem_base + 2 * kBN + g * D, tmem_base + g * kBN + kk * 8, sdesc_advance(va, kk * 2048), idesc_pv, 1u);
+                tc_commit(&bar_odone[g]);
             };
             FwdTiles<SINK> tiles(p, tile_begin, tile_end);
             FwdTile<SINK> x;
@@ -417,8 +464,8 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
                     if (last == top) tc_commit(bar_qempty);  // no later MMA of this tile reads Q
                     ++ring;
                     int jn = 0;
-                    for (int j = top; j >= last && ok; j = jn) {
-                        jn = SINK && j != last ? x.after(j, 0) : j - 1;
+                    for (int j = top; (SINK ? j >= 0 : j >= last) && ok; j = jn) {
+                        jn = x.after(j);
                         const uint32_t st_v = ring % L::kStages;
                         const uint32_t ph_v = (ring / L::kStages) & 1;
                         ++ring;
@@ -432,17 +479,23 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
                                 if (ok) ok = mbar_wait(&bar_ppart[g], pcnt[g] & 1, abort_flag);   // P of the first kPFirst keys
                                 if (!ok) break;
                                 tc_fence_after();
-                                issue_pv(g, st_v, j != x.hi[g], 0, kPFirst / 16);
+                                bool early = false;
+                                if constexpr (SINK) early = j < x.lo[g];
+                                if (!early) issue_pv(g, st_v, j != x.hi[g], 0, kPFirst / 16);
                                 ok = mbar_wait(&bar_pready[g], pcnt[g] & 1, abort_flag);  // the rest, while those MMAs run
                                 if (!ok) break;
                                 ++pcnt[g];
                                 tc_fence_after();
-                                issue_pv(g, st_v, j != x.hi[g], kPFirst / 16, kBN / 16);
+                                if (!early) issue_pv(g, st_v, j != x.hi[g], kPFirst / 16, kBN / 16);
+                                if constexpr (SINK) { if (early) issue_sink_pv(x, g, st_v, j); }
                             }
                             if (more && x.sees(g, jn)) {
                                 if (!have_k) { ok = mbar_wait(&bar_full[st_k], (ring / L::kStages) & 1, abort_flag); have_k = true; }
                                 if (!ok) break;
-                                issue_s(g, st_k);
+                                bool early = false;
+                                if constexpr (SINK) early = jn < x.lo[g];
+                                if (!early) issue_s(g, st_k);
+                                if constexpr (SINK) { if (early) issue_sink_s(x, g, st_k, jn); }
                             }
                         }
                         if (!ok) break;
@@ -511,7 +564,7 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
             for (int hh = 0; hh < heads_per_shard && ok; ++hh) {
                 const int h = (x.t % p.H) * heads_per_shard + hh;
                 float m_ref = -INFINITY, l_sum = 0.f;
-                for (int j = hi; (SINK ? j >= 0 : j >= lo) && ok; j = SINK ? x.after(j, g) : j - 1) {
+                for (int j = hi; j >= lo && ok; --j) {
                     ok = warp_wait(&bar_sfull[g], scnt & 1, abort_flag);
                     if (!ok) break;
                     ++scnt;
@@ -528,7 +581,7 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
                         const int c_hi = row_ok ? (int)(row - k0) : kBN;     // last visible column
 #pragma unroll
                         for (int w = 0; w < kBN / 32; ++w) {
-                            uint32_t vis = range_bits(c_lo - 32 * w, c_hi - 32 * w);
+                            uint32_t vis = range_bits(c_lo - 32 * w, c_hi - 32 * w);   // (a block of the window may hold sinks, too)
                             if (SINK) vis |= range_bits(sink_lo - k0 - 32 * w, sink_hi - k0 - 32 * w);
 #pragma unroll
                             for (int i = 0; i < 32; ++i) sr[32 * w + i] = (vis >> i) & 1u ? sr[32 * w + i] : 0xff800000u;  // -inf
@@ -590,6 +643,63 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
                     tc_fence_before();
                     mbar_arrive(&bar_pready[g]);
                     ++ocnt;
+                }
+                if constexpr (SINK) {   // the same for the blocks of sinks, a group of 32 columns at a time
+                    for (int j = x.shi[g]; j >= x.slo[g] && ok; --j) {
+                        ok = warp_wait(&bar_sfull[g], scnt & 1, abort_flag);
+                        if (!ok) break;
+                        ++scnt;
+                        tc_fence_after();
+                        int c0, c1;
+                        x.sink_groups(g, j, p.sinks, c0, c1);
+                        const int s_lo = sink_lo - j * kBN, s_hi = sink_hi - j * kBN;
+                        float mx = -INFINITY;
+#pragma unroll 1
+                        for (int c = c0; c <= c1; ++c) {
+                            uint32_t s[32];
+                            tmem_ld32(t_s + 32 * c, s);
+                            tmem_ld_wait();
+                            const uint32_t vis = range_bits(s_lo - 32 * c, s_hi - 32 * c);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) mx = fmaxf(mx, (vis >> i) & 1u ? __uint_as_float(s[i]) : -INFINITY);
+                        }
+                        mx *= p.scale_log2;
+                        float factor = 1.0f;
+                        if (mx > m_ref + kRescaleThreshold) {
+                            factor = ex2_approx(m_ref - mx);
+                            m_ref = mx;
+                        }
+                        if (__any_sync(0xffffffffu, factor != 1.0f)) {
+                            ok = rescale_o(factor);
+                            if (!ok) break;
+                        }
+                        l_sum *= factor;
+                        const float m_use = (m_ref == -INFINITY) ? 0.f : m_ref;
+                        // (P of group c lies over S of group c / 2, which has been read)
+#pragma unroll 1
+                        for (int c = c0; c <= c1; ++c) {
+                            uint32_t s[32], pk[16];
+                            tmem_ld32(t_s + 32 * c, s);
+                            tmem_ld_wait();
+                            const uint32_t vis = range_bits(s_lo - 32 * c, s_hi - 32 * c);
+                            float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2) {
+                                const float p0 = (vis >> i) & 1u ? ex2_approx(fmaf(__uint_as_float(s[i]), p.scale_log2, -m_use)) : 0.f;
+                                const float p1 = (vis >> (i + 1)) & 1u ? ex2_approx(fmaf(__uint_as_float(s[i + 1]), p.scale_log2, -m_use)) : 0.f;
+                                sum0 += p0;
+                                sum1 += p1;
+                                pk[i >> 1] = pack_bf16x2(p0, p1);
+                            }
+                            l_sum += sum0 + sum1;
+                            tmem_st16(t_s + 16 * c, pk);
+                        }
+                        tmem_st_wait();
+                        tc_fence_before();
+                        mbar_arrive(&bar_ppart[g]);
+                        mbar_arrive(&bar_pready[g]);
+                        ++ocnt;
+                    }
                 }
                 if (!ok) break;
                 // epilogue: wait for the last PV, normalise, store

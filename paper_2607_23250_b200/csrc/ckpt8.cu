@@ -4,44 +4,21 @@
 // Both directions are bound by memory: 2 bytes a value on one side, 33 / 32 on the other.  A warp takes kWarpRuns runs of 32
 // values: four lanes a run, 16 bytes of bf16 and 8 of integers a lane, all loads issued before the first is used, and
 // the runs' exponent bytes as one 32-byte access.  The tensors of a call share a launch.
-#include "ckpt8.cuh"
 #include "common.h"
+#include "ckpt8.cuh"
 
 namespace libra {
 
-constexpr int kSteps = 4;                       // runs a lane takes part in
-constexpr int kWarpRuns = 8 * kSteps;
 constexpr int kCkptThreads = 256;
 
-struct CkptTensor {
-    uint4* x;               // bf16, 8 values each
-    uint2* q;               // integers, 8 each
-    uint8_t* e;             // exponents
-    int64_t runs;
-    uint32_t chunks;        // warps' shares of it
-};
 struct CkptArgs {
     CkptTensor t[4];
-    const int* plan_status; // null, or non-zero there: do nothing
 };
-
-// The tensor of this warp's share and its first run (selected, not indexed: an index into the arguments would copy them to
-// local memory).
-__device__ __forceinline__ CkptTensor my_tensor(const CkptArgs& a, int64_t& run0) {
-    uint32_t w = blockIdx.x * (kCkptThreads / 32) + (threadIdx.x >> 5);
-    CkptTensor t = a.t[0];
-#pragma unroll
-    for (int k = 1; k < 4; ++k)
-        if (w >= t.chunks) { w -= t.chunks; t = a.t[k]; }
-    if (w >= t.chunks) t.runs = 0;
-    run0 = (int64_t)w * kWarpRuns;
-    return t;
-}
 
 __global__ void __launch_bounds__(kCkptThreads) k_ckpt8_pack(const __grid_constant__ CkptArgs a) {
     grid_dep_wait();
     int64_t run0;
-    const CkptTensor t = my_tensor(a, run0);
+    const CkptTensor t = share_of(a.t, blockIdx.x * (kCkptThreads / 32) + (threadIdx.x >> 5), run0);
     if (run0 >= t.runs) return;
     const int lane = threadIdx.x & 31;
     const int64_t at = run0 * 4 + lane;         // this lane's eight values of step 0
@@ -83,54 +60,16 @@ __global__ void __launch_bounds__(kCkptThreads) k_ckpt8_pack(const __grid_consta
 
 __global__ void __launch_bounds__(kCkptThreads) k_ckpt8_unpack(const __grid_constant__ CkptArgs a) {
     grid_dep_wait();
-    if (a.plan_status && *a.plan_status != 0) return;
-    int64_t run0;
-    const CkptTensor t = my_tensor(a, run0);
-    if (run0 >= t.runs) return;
-    const int lane = threadIdx.x & 31;
-    const int64_t at = run0 * 4 + lane;
-    uint2 q[kSteps];
-#pragma unroll
-    for (int u = 0; u < kSteps; ++u) {
-        q[u] = make_uint2(0, 0);
-        if (run0 + 8 * u + (lane >> 2) < t.runs) q[u] = __ldcs(t.q + at + 32 * u);
-    }
-    const uint32_t mine = run0 + lane < t.runs ? t.e[run0 + lane] : 7u;
-#pragma unroll
-    for (int u = 0; u < kSteps; ++u) {
-        const float up = run_up(__shfl_sync(0xffffffffu, mine, 8 * u + (lane >> 2)));
-        float f[8];
-        held_floats(q[u].x, f);
-        held_floats(q[u].y, f + 4);
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(f[2 * i] * up, f[2 * i + 1] * up);
-        if (run0 + 8 * u + (lane >> 2) < t.runs) t.x[at + 32 * u] = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-}
-
-// One tensor of a call: null everywhere = left out.  Returns false where only some of its pointers are given or misaligned.
-static bool set_tensor(CkptTensor& t, const void* x, const void* q, const void* e, int64_t values) {
-    t = {};
-    if (!x && !q && !e) return true;
-    if (!x || !q || !e || (((uintptr_t)x | (uintptr_t)q) & 15)) return false;
-    t.x = (uint4*)x;
-    t.q = (uint2*)q;
-    t.e = (uint8_t*)e;
-    t.runs = values / kRun;
-    t.chunks = (uint32_t)((t.runs + kWarpRuns - 1) / kWarpRuns);
-    return true;
+    unpack_share(a.t, blockIdx.x * (kCkptThreads / 32) + (threadIdx.x >> 5));
 }
 
 // pack: x -> held, else held -> x.
-static int run_ckpt8(bool pack, const void* const (&x)[4], const libra_ckpt8* c, const libra_dims* dims, const int* plan_status,
-                     cudaStream_t s) {
+static int run_ckpt8(bool pack, const void* const (&x)[4], const libra_ckpt8* c, const libra_dims* dims, cudaStream_t s) {
     if (!c || !dims || dims->total_tokens <= 0 || dims->hq <= 0 || dims->hkv <= 0) return LIBRA_ERR_INVALID_ARG;
     if (dims->head_dim != 64 && dims->head_dim != 128 && dims->head_dim != 256) return LIBRA_ERR_UNSUPPORTED;
     const void* const q[4] = {c->q, c->k, c->v, c->out};
     const void* const e[4] = {c->q_exp, c->k_exp, c->v_exp, c->out_exp};
     CkptArgs a = {};
-    a.plan_status = plan_status;
     int64_t warps = 0;
     for (int k = 0; k < 4; ++k) {
         const int heads = k == 0 || k == 3 ? dims->hq : dims->hkv;
@@ -149,20 +88,16 @@ static int run_ckpt8(bool pack, const void* const (&x)[4], const libra_ckpt8* c,
     return err == cudaSuccess ? LIBRA_OK : LIBRA_ERR_CUDA;
 }
 
-int launch_ckpt8_restore(const libra_ckpt8* c, void* q, void* k, void* v, const libra_dims* dims, const int* plan_status, cudaStream_t s) {
-    return run_ckpt8(false, {q, k, v, nullptr}, c, dims, plan_status, s);
-}
-
 }  // namespace libra
 
 using namespace libra;
 
 extern "C" int libra_ckpt8_pack(const void* q_dev, const void* k_dev, const void* v_dev, const void* out_dev,
                                 const libra_ckpt8* ckpt, const libra_dims* dims, void* stream) {
-    return run_ckpt8(true, {q_dev, k_dev, v_dev, out_dev}, ckpt, dims, nullptr, (cudaStream_t)stream);
+    return run_ckpt8(true, {q_dev, k_dev, v_dev, out_dev}, ckpt, dims, (cudaStream_t)stream);
 }
 
 extern "C" int libra_ckpt8_unpack(const libra_ckpt8* ckpt, void* q_dev, void* k_dev, void* v_dev, void* out_dev,
                                   const libra_dims* dims, void* stream) {
-    return run_ckpt8(false, {q_dev, k_dev, v_dev, out_dev}, ckpt, dims, nullptr, (cudaStream_t)stream);
+    return run_ckpt8(false, {q_dev, k_dev, v_dev, out_dev}, ckpt, dims, (cudaStream_t)stream);
 }

@@ -12,6 +12,7 @@
 #pragma once
 #include <stdint.h>
 
+#include "../../include/libra.h"
 #include "ptx.cuh"
 
 namespace libra {
@@ -29,6 +30,79 @@ __device__ __forceinline__ void held_floats(uint32_t w, float* f) {
     const uint32_t u = w ^ 0x80808080u;   // q + 128
 #pragma unroll
     for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7540 + i)) - 8388736.0f;
+}
+
+// How warps share a call's tensors: kWarpRuns runs of one of them each, four lanes a run, 16 bytes of bf16 and 8 of integers a
+// lane and step; the runs' exponents are one 32-byte access.
+constexpr int kSteps = 4;                       // runs a lane takes part in
+constexpr int kWarpRuns = 8 * kSteps;
+
+struct CkptTensor {
+    uint4* x;               // bf16, 8 values each
+    uint2* q;               // integers, 8 each
+    uint8_t* e;             // exponents
+    int64_t runs;
+    uint32_t chunks;        // warps' shares of it
+};
+
+// The tensor of warp w's share and its first run (selected, not indexed: an index into a kernel's arguments would copy them to
+// local memory).
+template <int N>
+__device__ __forceinline__ CkptTensor share_of(const CkptTensor (&all)[N], uint32_t w, int64_t& run0) {
+    CkptTensor t = all[0];
+#pragma unroll
+    for (int k = 1; k < N; ++k)
+        if (w >= t.chunks) { w -= t.chunks; t = all[k]; }
+    if (w >= t.chunks) t.runs = 0;
+    run0 = (int64_t)w * kWarpRuns;
+    return t;
+}
+// Reads warp w's share back as bf16.
+template <int N>
+__device__ __forceinline__ void unpack_share(const CkptTensor (&all)[N], uint32_t w_) {
+    int64_t run0;
+    const CkptTensor t = share_of(all, w_, run0);
+    if (run0 >= t.runs) return;
+    const int lane = threadIdx.x & 31;
+    const int64_t at = run0 * 4 + lane;
+    uint2 q[kSteps];
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) {
+        q[u] = make_uint2(0, 0);
+        if (run0 + 8 * u + (lane >> 2) < t.runs) q[u] = __ldcs(t.q + at + 32 * u);
+    }
+    const uint32_t mine = run0 + lane < t.runs ? t.e[run0 + lane] : 7u;
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) {
+        const float up = run_up(__shfl_sync(0xffffffffu, mine, 8 * u + (lane >> 2)));
+        float f[8];
+        held_floats(q[u].x, f);
+        held_floats(q[u].y, f + 4);
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(f[2 * i] * up, f[2 * i + 1] * up);
+        if (run0 + 8 * u + (lane >> 2) < t.runs) t.x[at + 32 * u] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// One tensor of a call: null everywhere = left out.  Returns false where only some of its pointers are given or misaligned.
+inline bool set_tensor(CkptTensor& t, const void* x, const void* q, const void* e, int64_t values) {
+    t = {};
+    if (!x && !q && !e) return true;
+    if (!x || !q || !e || (((uintptr_t)x | (uintptr_t)q) & 15)) return false;
+    t.x = (uint4*)x;
+    t.q = (uint2*)q;
+    t.e = (uint8_t*)e;
+    t.runs = values / kRun;
+    t.chunks = (uint32_t)((t.runs + kWarpRuns - 1) / kWarpRuns);
+    return true;
+}
+
+// q, k and v of a checkpoint and where they are restored.
+inline bool set_restore(CkptTensor (&t)[3], const libra_ckpt8* c, void* q, void* k, void* v, const libra_dims* dims) {
+    const int64_t row = dims->total_tokens * dims->head_dim;
+    return set_tensor(t[0], q, c->q, c->q_exp, row * dims->hq) && set_tensor(t[1], k, c->k, c->k_exp, row * dims->hkv) &&
+           set_tensor(t[2], v, c->v, c->v_exp, row * dims->hkv);
 }
 
 }  // namespace libra

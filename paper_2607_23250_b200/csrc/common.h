@@ -38,6 +38,9 @@ struct PlanDir {
     // plans with sinks: the key blocks ahead of first_j that rows of the chunk see all the same (pair-blocks base .. base + n - 1)
     int32_t* d_sink_j = nullptr;       // [chunks] first of them
     int32_t* d_sink_n = nullptr;       // [chunks] their number
+    // key-major tiles with the sinks' tails apart (direction 5): key block, first row block, row blocks, slot of partial sums
+    int4* d_units = nullptr;           // [NB]
+    int n_tails = 0, tail_width = 0, tail_rows = 0;   // the last n_tails units, tail_width of them for each chunk of tail_rows row blocks
 };
 
 }  // namespace libra
@@ -58,8 +61,8 @@ struct libra_plan {
     int32_t* d_tok_start = nullptr;  // [T] first key that query t sees, the sinks ahead of its window left out
     int32_t* d_tok_end = nullptr;    // [T] one past the last query that sees key t
     int32_t* d_tok_first = nullptr;  // [T] first token of the sample that holds token t; plans with sinks only
-    int32_t* d_blk_end = nullptr;    // [ceil(T / 128)] the largest tok_end among the block's keys
-    int32_t* d_blk_min = nullptr;    // [ceil(T / 128)] at most the smallest of them
+    int2* d_blk = nullptr;           // [ceil(T / 128)] of the block's keys at most the smallest tok_end, and the largest
+    int32_t* d_blk_near = nullptr;   // [ceil(T / 128)] the end of the queries whose windows hold one of them; plans with sinks only
     int* d_status = nullptr;         // the planner's verdict on cu_seqlens
     // Outcome of each CTA of the last launch of a kernel (0 or LIBRA_ERR_*), written by every CTA when it leaves, so
     // that nothing has to be cleared before a launch: forward; dK/dV, fused or dV pass; dK pass; dQ kernel or pass.
@@ -69,8 +72,9 @@ struct libra_plan {
     int bwd_mask = 0;                // which of d_outcome[1..3] the last backward wrote
     // 0 = query-major, 1 = key-major, 2 = pair tiles (key block x query chunk), 3 = the key-stationary tiles of kernels that
     // run on pairs of CTAs: as 2 when that is there, else as 1, with 256 keys a tile and a worker for every two; 4 = the pair
-    // tiles of the fused kernel on pairs of CTAs, 256 keys a tile and the query chunks of 2
-    static constexpr int kDirs = 5;
+    // tiles of the fused kernel on pairs of CTAs, 256 keys a tile and the query chunks of 2; 5 = as 1 with a window and sinks:
+    // what a key block that holds sinks is seen by beyond its window is cut into tiles of their own
+    static constexpr int kDirs = 6;
     libra::PlanDir dir[kDirs];
     uint32_t wait_limit_ns = 2000000000u;  // budget of one device-side wait (libra_plan_set_wait_limit_ns)
     int inject_stall = 0;            // test aid: the producer role issues no loads (libra_plan_inject_stall)
@@ -115,8 +119,6 @@ namespace libra {
 int make_thd_map(CUtensorMap* m, const void* base, int64_t T, int H, int d, int box_rows);
 // fp32 tensor [T, H, d] viewed as (d, H, T); box = box_cols x 1 x box_rows, 128-byte swizzle.
 int make_f32_3d_map(CUtensorMap* m, const void* base, int64_t T, int H, int d, int box_cols, int box_rows);
-// q, k, v of a checkpoint as bf16 (ckpt8.cu); nothing where *plan_status is not 0.
-int launch_ckpt8_restore(const libra_ckpt8* c, void* q, void* k, void* v, const libra_dims* dims, const int* plan_status, cudaStream_t s);
 // head_dim 256 (attn_d256.cu): the forward over the plan's query-major lists; the three gradient passes over
 // its key-major (dV, dK) and query-major (dQ) lists, given the row statistics lse2 / dvec [Hq, Tpad].
 int launch_fwd_d256(const void* q, const void* k, const void* v, void* out, float* lse, const libra_plan* plan,
@@ -134,14 +136,14 @@ int launch_bwd_d256(const void* q, const void* k, const void* v, const void* dou
 // ahead had itself waited for, before it ends.  A step on 10007 tokens (forward, statistics, fused backward,
 // conversion): 175 -> 153 us with the clearing of accumulators and status words moved into those kernels.
 template <unsigned CLUSTER = 1, typename... KArgs, typename... Args>
-static inline cudaError_t launch_dependent(void (*kernel)(KArgs...), unsigned grid, unsigned block, size_t smem, cudaStream_t s,
+static inline cudaError_t launch_dependent(void (*kernel)(KArgs...), dim3 grid, unsigned block, size_t smem, cudaStream_t s,
                                            const Args&... args) {
     cudaLaunchAttribute attrs[2] = {};
     cudaLaunchAttribute& attr = attrs[0];
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(block);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;

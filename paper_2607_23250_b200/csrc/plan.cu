@@ -82,7 +82,8 @@ cudaError_t scratch_alloc(void** p, size_t bytes, cudaStream_t s) {
 // start <= t < end <= T, so that a malformed cu_seqlens (flagged in *status) can never make a
 // later kernel form an address outside its tensors.
 struct TokenBounds {
-    int32_t *tok_start, *tok_end, *tok_first, *blk_end, *blk_min;   // tok_first: null without sinks
+    int32_t *tok_start, *tok_end, *tok_first, *blk_near;   // tok_first, blk_near: null without sinks
+    int2* blk;                                              // smallest and largest end
     int64_t window, sinks;                                          // window: T where there is none
 };
 __global__ void k_token_bounds(const int32_t* __restrict__ cu, int n, int64_t T, const TokenBounds out, int* status) {
@@ -107,8 +108,9 @@ __global__ void k_token_bounds(const int32_t* __restrict__ cu, int n, int64_t T,
     out.tok_start[t] = (int32_t)(t - out.window + 1 > a ? t - out.window + 1 : a);
     out.tok_end[t] = (int32_t)(t - a < out.sinks ? e : near);
     if (out.tok_first) out.tok_first[t] = (int32_t)a;
-    if (t % 128 == 0) out.blk_min[t / 128] = (int32_t)near;
-    if (t % 128 == 127 || t == T - 1) out.blk_end[t / 128] = (int32_t)(a + out.sinks > t / 128 * 128 ? e : near);
+    if (t % 128 == 0) out.blk[t / 128].x = (int32_t)near;
+    if (out.blk_near && (t % 128 == 127 || t == T - 1)) out.blk_near[t / 128] = (int32_t)near;
+    if (t % 128 == 127 || t == T - 1) out.blk[t / 128].y = (int32_t)(out.sinks > 0 && a + out.sinks > t / 128 * 128 ? e : near);
 }
 
 // The mask as the planning kernels see it.
@@ -150,6 +152,7 @@ struct DirView {
     int32_t* cta_tiles;
     int32_t* cta_exec;
     int64_t* loads;
+    int4* units;            // null: blocks of `tile` tokens
 };
 struct DirViews {
     DirView v[libra_plan::kDirs];
@@ -171,7 +174,7 @@ __global__ void k_block_weights(const MaskView m, const DirViews views) {
     const int64_t T = m.T;
     const int64_t b = (blockIdx.x * (int64_t)blockDim.x + threadIdx.x) >> 5;
     const int lane = threadIdx.x & 31;
-    if (b >= d.NB) return;
+    if (b >= d.NB || d.units) return;
     const int64_t t0 = b * d.tile;
     const int64_t t1 = (t0 + d.tile < T) ? t0 + d.tile : T;
     int64_t w = 0;
@@ -207,6 +210,42 @@ __global__ void k_block_weights(const MaskView m, const DirViews views) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
     if (lane == 0) d.weight_blk[b] = w;
+}
+
+// Key-major tiles of plans with sinks (direction 5; the two-kernel backward).  A key block that holds sinks of a long sample is
+// seen by all of it: one tile a block, as the exported lists have it, made that tile the launch (16000 tokens in one sample, 8 / 2
+// heads of 64, window 1001: 500 row blocks of the 68 that a CTA has on average, 899 us).  So of such a block the row blocks up to the
+// end of the chunk of R in which its window ends are the main tile, and those of each later chunk are a tile of their own.
+// Chunk c holds such a tail of key block j when its first row sees a sink there, but no key by its window; the blocks
+// of which that is true are neighbours and at most `width`.  Unit NB + c width + x is the tail of the x-th of them, empty where
+// there are fewer.  The partial sums of main tile and tails have slots of their own (w; -1: none, the results are stored) and are added up
+// in the order of the chunks, so that the result does not depend on the schedule.
+__global__ void k_tail_units(const MaskView m, const int2* __restrict__ blk, const int32_t* __restrict__ blk_near,
+                             int64_t n_main, int R, int width, const DirView d) {
+    const int64_t u = blockIdx.x * (int64_t)blockDim.x + threadIdx.x;
+    if (u >= d.NB) return;
+    const int n_tails = (int)(d.NB - n_main);
+    int4 unit = make_int4(0, 0, 0, -1);
+    if (u < n_main) {
+        const int j = (int)u, last = (blk[j].y - 1) / 128, c = (blk_near[j] - 1) / 128 / R;
+        const int end = last < c * R + R - 1 ? last : c * R + R - 1;
+        unit = make_int4(j, j, end - j + 1, -1);
+        if (last > end) {   // the first tail's number names the slot
+            const int x = j - m.tok_first[(int64_t)(c + 1) * R * 128] / 128;
+            unit.w = x >= 0 && x < width ? (c + 1) * width + x : -1;   // (out of range: a malformed cu_seqlens, nothing will run)
+        }
+    } else {
+        const int idx = (int)(u - n_main), c = idx / width;
+        const int64_t t0 = (int64_t)c * R * 128, a = m.tok_first[t0], j = a / 128 + idx % width;
+        const int64_t e = a + m.sinks < t0 ? a + m.sinks : t0;
+        if (j * 128 < e && (blk_near[j] - 1) / 128 / R < c) {
+            const int last = (blk[j].y - 1) / 128, end = last < c * R + R - 1 ? last : c * R + R - 1;
+            unit = make_int4((int)j, c * R, end - c * R + 1, n_tails + idx);
+        }
+    }
+    if (unit.z < 0) unit.z = 0;
+    d.units[u] = unit;
+    d.weight_blk[u] = unit.z ? 8 * unit.z + d.unit_cost : 0;
 }
 
 // Order of Algorithm 2: decreasing weight, then increasing id.  All H shards of a block weigh
@@ -528,6 +567,7 @@ static void carve_dir(PlanDir& d, Carver& c, bool zeros, bool pairs) {
         return;
     }
     c.take(&d.d_weight_blk, d.NB);
+    if (d.tail_width) c.take(&d.d_units, d.NB);
     if (!pairs) c.take(&d.d_blk_order, d.NB);
     c.take(&d.d_cta_of_tile, d.NT);
     c.take(&d.d_pos, d.NT);
@@ -561,6 +601,7 @@ static DirView view_of(const PlanDir& d, int key_major, const libra_plan_opts& o
     v.unit_cost = key_major ? o.unit_cost_kv : o.unit_cost_q;
     v.weight_blk = d.d_weight_blk; v.blk_order = d.d_blk_order; v.cta_of_tile = d.d_cta_of_tile; v.pos = d.d_pos;
     v.cta_offsets = d.d_cta_offsets; v.cta_tiles = d.d_cta_tiles; v.cta_exec = d.d_cta_exec; v.loads = d.d_loads;
+    v.units = d.d_units;
     return v;
 }
 
@@ -592,7 +633,15 @@ static const PairTables* choose_pair_chunk(const libra_plan* p, const PairCands&
         const PairTables& t = cands.c[x];
         if (t.dir != k || totals[x] > 262144) continue;
         const double longest = (double)totals[kPairCands + k - 2];
-        const double cost = 3.0 * totals[x] * p->dir[k].H / p->dir[k].W + G * (t.R < longest ? t.R : longest);
+        double cost = 3.0 * totals[x] * p->dir[k].H / p->dir[k].W + G * (t.R < longest ? t.R : longest);
+        if (p->sinks) {
+            // Tiles as long as a chunk are few, those of key blocks with sinks, and come first of a chunk's: the others bound
+            // the end, unless one tile is the launch.
+            const double usual = p->window / t.kt + 2, cells = G * totals[kPairCands + 2 + k - 2] * p->dir[k].H / p->dir[k].W;
+            const double tile = 3.0 + G * (t.R < longest ? t.R : longest);
+            cost = cells + 3.0 * totals[x] * p->dir[k].H / p->dir[k].W + G * (t.R < usual ? t.R : usual);
+            if (cost < tile) cost = tile;
+        }
         if (!best || cost < least) { best = &t; least = cost; }
     }
     return best;
@@ -675,11 +724,25 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
     const int64_t T = p->T;
     cudaStream_t s = p->stream;
     const bool wide_pairs = want[3] && want[2];                   // the wide tiles are pair tiles
-    const bool sorted[kDirs] = {want[0], want[1], false, want[3] && !want[2], false};   // sizes known, placed heaviest first
-    bool pairs[kDirs] = {false, false, want[2], wide_pairs, want[4]};
+    const bool sorted[kDirs] = {want[0], want[1], false, want[3] && !want[2], false, want[5]};   // sizes known, placed heaviest first
+    bool pairs[kDirs] = {false, false, want[2], wide_pairs, want[4], false};
     for (int k = 0; k < kDirs; ++k) {
         if (!sorted[k]) continue;
         p->dir[k].NB = (T + p->dir[k].tile - 1) / p->dir[k].tile;
+        if (k == 5) {
+            // Chunks of about half a window: a tail then weighs no more than other tiles.  Not so many of them that the slots of
+            // partial sums, 2 x 64 KB a tail and kv head at head_dim 64, are more than a few hundred.
+            PlanDir& d = p->dir[k];
+            const int64_t width = (p->sinks + 126) / 128 + 1, rows = (p->window / 128 + 1) / 2;
+            int64_t R = rows > 8 ? rows : 8;
+            R = R > width ? R : width;
+            const int64_t least = width < 4 ? (d.NB + 63) / 64 : (d.NB * width + 255) / 256;
+            R = R > least ? R : least;
+            d.tail_rows = (int)R;
+            d.tail_width = (int)width;
+            d.n_tails = (int)((d.NB + R - 1) / R * width);
+            d.NB += d.n_tails;
+        }
         if (const int rc = check_dir(p, p->dir[k], false); rc != LIBRA_OK) return rc;
     }
     PairCands cands;
@@ -705,9 +768,8 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
         zero_bytes = c.used;
         c.take(&p->d_tok_start, T);
         c.take(&p->d_tok_end, T);
-        if (p->sinks) c.take(&p->d_tok_first, T);
-        c.take(&p->d_blk_end, (T + 127) / 128);
-        c.take(&p->d_blk_min, (T + 127) / 128);
+        if (p->sinks) { c.take(&p->d_tok_first, T); c.take(&p->d_blk_near, (T + 127) / 128); }
+        c.take(&p->d_blk, (T + 127) / 128);
         for (int k = 0; k < kDirs; ++k)
             if (sorted[k]) carve_dir(p->dir[k], c, false, false);
         if (want[2]) {
@@ -728,7 +790,7 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
     cudaMemsetAsync(mem.at, 0, zero_bytes, s);
     const int64_t span = T > p->n + 1 ? T : p->n + 1;
     const int64_t window = p->window ? p->window : T;
-    const TokenBounds bounds = {p->d_tok_start, p->d_tok_end, p->d_tok_first, p->d_blk_end, p->d_blk_min, window, p->sinks};
+    const TokenBounds bounds = {p->d_tok_start, p->d_tok_end, p->d_tok_first, p->d_blk_near, p->d_blk, window, p->sinks};
     const MaskView mask = {p->d_tok_start, p->d_tok_end, p->d_tok_first, T, window, p->sinks};
     k_token_bounds<<<grid_for(span, 256), 256, 0, s>>>(cu, p->n, T, bounds, p->d_status);
     count_launch();
@@ -775,6 +837,12 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
             max_nb = p->dir[k].NB > max_nb ? p->dir[k].NB : max_nb;
         }
     if (n > 0) {
+        if (sorted[5]) {
+            const PlanDir& d = p->dir[5];
+            k_tail_units<<<grid_for(d.NB, 256), 256, 0, s>>>(mask, p->d_blk, p->d_blk_near, d.NB - d.n_tails, d.tail_rows, d.tail_width,
+                                                             views.v[n - 1]);
+            count_launch();
+        }
         k_block_weights<<<dim3(grid_for(max_nb * 32, 256), n), 256, 0, s>>>(mask, views);
         k_rank_blocks<<<dim3(grid_for(max_nb, 16), n), 256, 0, s>>>(views);
         count_launch(2);
@@ -782,7 +850,7 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
     const int n_sorted = n;
     // No kernel walks the lists of the 128-key pair tiles where the fused backward has its wide ones: they are made when they
     // are exported.
-    const bool listed[kDirs] = {sorted[0], sorted[1], pairs[2] && !pairs[4], sorted[3] || pairs[3], pairs[4]};
+    const bool listed[kDirs] = {sorted[0], sorted[1], pairs[2] && !pairs[4], sorted[3] || pairs[3], pairs[4], sorted[5]};
     for (int k = 2; k < kDirs; ++k)
         if (listed[k] && !sorted[k]) views.v[n++] = view_of(p->dir[k], 1, o);
     if (n == 0) return LIBRA_OK;
@@ -811,6 +879,9 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
 }  // namespace libra
 
 using namespace libra;
+
+// Unit costs of windowed plans' block counts, in eighths of a block.
+constexpr int kWindowCostQ = 12, kWindowCostKv = 6;
 
 // window = 0: none.
 static int make_plan(const int32_t* cu_seqlens_dev, int n_samples, int n_heads, int tile_q, const libra_plan_opts* opts, int window,
@@ -846,19 +917,29 @@ static int make_plan(const int32_t* cu_seqlens_dev, int n_samples, int n_heads, 
     if (s) p->other_stream = 1;
     p->window = window < T ? window : 0;                 // (every query sees all of its sample then, the sinks too)
     p->sinks = p->window ? (sinks < T ? sinks : (int)T) : 0;
+    if (p->window && o.weight_model == LIBRA_WEIGHT_PAIRS) {
+        // Visible pairs say too little of a tile's time here: a tile of short samples has a fiftieth of a full one's pairs and
+        // an eighth of its blocks, and one worker got fifty of them (dK/dV of 131072 tokens, 4 / 1 heads, window 1024: 2.6 times the
+        // mean busy time).
+        o.weight_model = LIBRA_WEIGHT_BLOCKS;
+        o.cost_block = 128;
+        o.unit_cost_q = kWindowCostQ;
+        o.unit_cost_kv = kWindowCostKv;
+    }
     p->W = o.n_workers ? o.n_workers : sms;
     const int dirs = o.directions ? o.directions : (LIBRA_DIR_Q | LIBRA_DIR_KV);
     const int tile_kv = o.tile_kv ? o.tile_kv : 128;
     const bool keys = (dirs & (LIBRA_DIR_KV | LIBRA_DIR_PAIR)) != 0;
     const bool want[libra_plan::kDirs] = {(dirs & LIBRA_DIR_Q) != 0, (dirs & LIBRA_DIR_KV) != 0, (dirs & LIBRA_DIR_PAIR) != 0,
                                           keys && tile_kv == 128,
-                                          (dirs & LIBRA_DIR_PAIR) != 0 && tile_kv == 128 && p->W >= 2};
+                                          (dirs & LIBRA_DIR_PAIR) != 0 && tile_kv == 128 && p->W >= 2,
+                                          (dirs & LIBRA_DIR_KV) != 0 && tile_kv == 128 && p->sinks > 0};
     for (int k = 0; k < libra_plan::kDirs; ++k) {
         PlanDir& d = p->dir[k];
-        d.tile = k == 0 ? tile_q : (k >= 3 ? 256 : tile_kv);
+        d.tile = k == 0 ? tile_q : (k == 3 || k == 4 ? 256 : tile_kv);
         d.H = k == 0 ? n_heads : (o.n_heads_kv ? o.n_heads_kv : n_heads);
         d.W = k == 3 ? (p->W + 1) / 2 : (k == 4 ? p->W / 2 : p->W);
-        d.chunk = k >= 2 ? (o.pair_chunk ? o.pair_chunk : 4096) : 0;
+        d.chunk = k >= 2 && k <= 4 ? (o.pair_chunk ? o.pair_chunk : 4096) : 0;
         if (k == 3) {
             // The 256-wide kernels go through a tile's heads one after the other and their workers are out of step, so what
             // the workers of a query chunk read lies anywhere in its Q and dO of a kv head's group: 1 KB a row and head,

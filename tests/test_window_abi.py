@@ -42,8 +42,8 @@ def test_reference_gradients_against_differences():
             assert abs((vals[0] - vals[1]) / (2 * eps) - float(dx[at])) < 1e-7 * (1 + abs(float(dx[at])))
 
 
-def test_weights_of_a_full_window_are_the_causal_ones():
-    cu = pools.cu_seqlens([4, 1, 7])
-    see = ref.visible(cu, 12, 0)
-    assert ref.tile_weights(see, 12, False) == [10 + 1 + 28] and ref.tile_weights(see, 5, True) == [11, 25, 3]
-    assert np.array_equal(see.numpy(), ref.visible(cu, 0, 0).numpy())
+def test_weights_by_hand():
+    see = ref.visible(pools.cu_seqlens([4, 1, 7]), 2, 1)     # chunks of 4: rows 8-11 see chunk 2, the last of chunk 1, the sink in 1
+    assert ref.tile_weights(see, 8, False, 4, 1) == [(8 + 1) + (8 + 1), 8 * 2 + 1]
+    assert ref.tile_weights(see, 4, True, 4, 0) == [8, 16, 8]
+    assert np.array_equal(ref.visible([0, 12], 12, 0).numpy(), ref.visible([0, 12], 0, 0).numpy())

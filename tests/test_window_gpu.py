@@ -111,16 +111,33 @@ def test_a_window_that_reaches_everything_changes_nothing(d, fused):
     cu = pools.cu_seqlens([300, 1, 800, 77])
     q, k, v, dout = _tensors(cu, 4, 2, d, 9)
     full = _plan(cu, 4, 2, fused, 0, 0)
-    wide = _plan(cu, 4, 2, fused, 800, 0)
-    a, b = (_run(p, q, k, v, dout, fused) for p in (full, wide))
-    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
-    if not fused:
-        assert all(torch.equal(x, y) for x, y in zip(a[2], b[2]))
+    longest = _plan(cu, 4, 2, fused, 800, 0)
+    wide = _plan(cu, 4, 2, fused, int(cu[-1]), 3)
+    a, b, c = (_run(p, q, k, v, dout, fused) for p in (full, longest, wide))
+    for x in (b, c):
+        assert torch.equal(a[0], x[0]) and torch.equal(a[1], x[1])
+        if not fused:
+            assert all(torch.equal(g, h) for g, h in zip(a[2], x[2]))
     for direction in ((lb.LIBRA_DIR_Q, lb.LIBRA_DIR_PAIR) if fused else (lb.LIBRA_DIR_Q, lb.LIBRA_DIR_KV)):
         x, y = full.export(direction), wide.export(direction)
         assert all(np.array_equal(x[key], y[key]) for key in x)
-    full.destroy()
-    wide.destroy()
+    for p in (full, longest, wide):
+        p.destroy()
+
+
+@pytest.mark.parametrize("window,sinks", [(200, 1), (130, 130), (90, 300), (1, 128), (2000, 4), (128, 700)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_tails_of_sinks_in_the_two_kernel_form(d, window, sinks):
+    """Key blocks with sinks whose row blocks beyond the window are tiles of their own, in one chunk and in several, of samples
+    that start in the same key block as others and of one that ends inside a chunk; the same bits twice."""
+    cu = pools.cu_seqlens([100, 20, 4500, 40, 2600, 7])
+    q, k, v, dout = _tensors(cu, 2, 1, d, window)
+    plan = _plan(cu, 2, 1, False, window, sinks)
+    got = _run(plan, q, k, v, dout, False)
+    _check(cu, q, k, v, dout, got, window, sinks)
+    again = _run(plan, q, k, v, dout, False)
+    assert all(torch.equal(x, y) for x, y in zip(got[2], again[2]))
+    plan.destroy()
 
 
 @pytest.mark.parametrize("seed", range(10))
@@ -140,13 +157,12 @@ def test_plan_weights_placement_and_pair_tiles(seed):
     assert plan.status() == 0
     for direction, heads, size, unit in ((lb.LIBRA_DIR_Q, H, tile, 5), (lb.LIBRA_DIR_KV, Hkv, tile_kv, 3)):
         got = plan.export(direction)
-        want = ref.tile_weights(see, size, direction == lb.LIBRA_DIR_KV, g, unit)
+        if not g:
+            unit = 12 if direction == lb.LIBRA_DIR_Q else 6            # the library's own
+        want = ref.tile_weights(see, size, direction == lb.LIBRA_DIR_KV, g or 128, unit)
         assert got["weight"].tolist() == [w for w in want for _ in range(heads)]
         cta, loads = ref.place(want, heads, W)
         assert np.array_equal(got["cta_of_tile"], cta) and np.array_equal(got["loads"], loads)
-    if not g:
-        q_w, kv_w = (plan.export(x)["weight"].sum() for x in (lb.LIBRA_DIR_Q, lb.LIBRA_DIR_KV))
-        assert q_w == H * int(see.sum()) and kv_w == Hkv * int(see.sum())
     want = ref.live_pairs(see, tile_kv, chunk)
     kb, qc, size = plan.export_pairs()
     assert size == chunk

@@ -81,16 +81,13 @@ def worst(got, want, bound):
 
 # ---- planning ---------------------------------------------------------------------------------------------
 
-def tile_weights(see, tile, key_major, cost_block=0, unit_cost=0):
-    """Weights of the blocks of `tile` tokens of one head shard, by counting on the mask."""
+def tile_weights(see, tile, key_major, cost_block, unit_cost=0):
+    """Block-count weights of the blocks of `tile` tokens of one head shard, by counting on the mask."""
     m = see.numpy().T if key_major else see.numpy()
     T = m.shape[0]
     out = []
     for t0 in range(0, T, tile):
         t1 = min(T, t0 + tile)
-        if not cost_block:
-            out.append(int(m[t0:t1].sum()))
-            continue
         w = 0
         for c in range(t0 // cost_block, (t1 - 1) // cost_block + 1):
             rows = m[max(t0, c * cost_block):min(t1, (c + 1) * cost_block)].any(0)
