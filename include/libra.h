@@ -143,6 +143,9 @@ int libra_plan_tiles(const int32_t* cu_seqlens_dev, int n_samples, int n_heads, 
  * hold the sinks of its first row's sample, then the others, ascending.  (With sinks the two-kernel backward at head_dim 64 and
  * 128 walks lists of its own instead of the key-major ones, in which the row blocks beyond the window of a key block that
  * holds sinks are tiles of their own; their partial sums are added up in a fixed order, in its workspace.)
+ * At head_dim 128 a plan with LIBRA_DIR_PAIR and LIBRA_DIR_Q leaves the backward's form to the library: the two-kernel form
+ * (bit-reproducible, and without the fp32 accumulators in the workspace) where short windows make it the faster one,
+ * libra_plan_fused_ctas then returns 0.
  * A window that is not below T gives what libra_plan_tiles gives, one that is not below any sample's length the same
  * results (with sinks up to rounding).  As there, an infinity or
  * a NaN of a key or value reaches rows that do not see it where they share a 128-row block with rows, and a key
@@ -189,7 +192,7 @@ int libra_plan_export_pairs(const libra_plan_t* plan, int32_t* key_block_host, i
                             int* chunk_tokens_host);
 
 /* CTAs that take a pair tile together in this plan's fused backward (head_dim 128): 1, or 2 where it runs on pairs of CTAs
- * (see libra_attn_pool_bwd).  Host value, no synchronisation.  Errors (negative): INVALID_ARG, PLAN_MISMATCH (no pair
+ * (see libra_attn_pool_bwd); 0: a windowed plan whose backward takes the two-kernel form.  Host value, no synchronisation.  Errors (negative): INVALID_ARG, PLAN_MISMATCH (no pair
  * tiles). */
 int libra_plan_fused_ctas(const libra_plan_t* plan);
 

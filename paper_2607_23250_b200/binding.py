@@ -135,7 +135,8 @@ class Plan:
         return kb, qc, chunk.value
 
     def fused_ctas(self) -> int:
-        """CTAs that take a pair tile together in the fused backward: 1, or 2 where it runs on pairs of CTAs."""
+        """CTAs that take a pair tile together in the fused backward: 1, or 2 where it runs on pairs of CTAs; 0: a windowed
+        plan whose backward takes the two-kernel form."""
         n = int(_lib.libra_plan_fused_ctas(self._h))
         _check(min(n, 0), "libra_plan_fused_ctas")
         return n

@@ -121,11 +121,11 @@ __device__ __forceinline__ int share_begin(int n_it, uint32_t rank, uint32_t siz
 
 // End of a tile that a cluster shares, for a thread of an exp group: group 0 finishes dK, group 1 dV.  Every CTA gives the
 // others the columns that they finish, D / size each, and adds up the partial sums of its own in the order of the ranks
-// (the result does not depend on which is ready first).  t_acc: the group's accumulator, gdst: the key's row or null.
-// Returns false on a timeout.
-template <int D>
+// (the result does not depend on which is ready first).  t_acc: the group's accumulator, gdst: the key's row or null; TAILS:
+// fdst, its row of partial sums, or null.  Returns false on a timeout.
+template <int D, bool TAILS>
 __device__ __noinline__ bool finish_shared(uint8_t* smem, uint64_t* bar_spent, uint32_t t_acc, int n_it, float mul,
-                                           __nv_bfloat16* gdst, volatile int* abort_flag) {
+                                           __nv_bfloat16* gdst, volatile int* abort_flag, float* fdst = nullptr) {
     const uint32_t size = cluster_size(), rank = cluster_rank();
     uint64_t* bar_partial = bar_spent + 1;
     const int grp = threadIdx.x >> 7, row = threadIdx.x & 127, lane = threadIdx.x & 31, n = D / (int)size;
@@ -175,7 +175,10 @@ __device__ __noinline__ bool finish_shared(uint8_t* smem, uint64_t* bar_spent, u
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += __uint_as_float(v[i]);
         }
-        if (gdst) {
+        if (TAILS && fdst) {
+            *reinterpret_cast<float4*>(fdst + rank * n + c) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+            *reinterpret_cast<float4*>(fdst + rank * n + c + 4) = make_float4(sum[4], sum[5], sum[6], sum[7]);
+        } else if (gdst) {
             uint4 w;
             w.x = pack_bf16x2(sum[0] * mul, sum[1] * mul);
             w.y = pack_bf16x2(sum[2] * mul, sum[3] * mul);
@@ -191,8 +194,8 @@ __device__ __noinline__ bool finish_shared(uint8_t* smem, uint64_t* bar_spent, u
 // fewer tiles than SMs the longest, G heads times the blocks of its sample, is the launch.  Step with one CTA a tile and with several: 2000 tokens, 8 /
 // 2 heads of 64: 104.6 -> 65.8 us (4 CTAs); 4000 tokens in one sample, 4 / 1 heads of 128: 237.9 -> 146.4 (4); 1500 tokens, 4 /
 // 1 heads: 96.8 -> 60.4 (8); 9000 tokens: 236.9 -> 162.3 (2).
-// TAILS (plans with sinks, not shared): the units are those of direction 5 (k_tail_units in plan.cu); some leave partial sums
-// in fp32, which k_sum_tails adds up.
+// TAILS (plans with sinks): the units are those of direction 5 (k_tail_units in plan.cu), some of them empty; some leave partial
+// sums in fp32, which k_sum_tails adds up.
 template <int D, bool SHARE, bool TAILS>
 __global__ void __launch_bounds__(kBwdThreads, 1)
 k_attn_bwd_dkdv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
@@ -604,8 +607,11 @@ k_attn_bwd_dkdv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             tc_fence_after();
             if constexpr (SHARE) {
                 __nv_bfloat16* gdst = (grp == 0 ? p.dk : p.dv) + ((size_t)key * p.hkv + kvh) * D;
-                const bool done = finish_shared<D>(smem, bar_spent, tmem_base + lane_addr + (grp == 0 ? kColDK : kColDV), G * nblk,
-                                                   grp == 0 ? p.scale : 1.0f, key_ok ? gdst : nullptr, abort_flag);
+                float* fdst = nullptr;
+                if constexpr (TAILS)
+                    if (slot >= 0) fdst = p.partial + ((((size_t)slot * p.hkv + kvh) * 2 + grp) * 128 + r) * D;
+                const bool done = finish_shared<D, TAILS>(smem, bar_spent, tmem_base + lane_addr + (grp == 0 ? kColDK : kColDV), G * nblk,
+                                                          grp == 0 ? p.scale : 1.0f, key_ok ? gdst : nullptr, abort_flag, fdst);
                 ok = __all_sync(0xffffffffu, done);
                 break;
             }
@@ -780,31 +786,34 @@ __global__ void k_bwd_prep(const void* __restrict__ out_, const uint8_t* __restr
 
 // Adds up the partial sums of key blocks with tails (dkdv kernel with TAILS), main tile first, then the chunks in order.  Block x: the
 // tail unit of that number, at work where that is the first tail of its key block; the others are `width` apart.  A thread has
-// four columns of a key; few blocks are at work, so the loads of a sum are issued eight at a time (65536 tokens in one sample, 32 / 4
+// four columns of a key (kt of them); few blocks are at work, so the loads of a sum are issued eight at a time (65536 tokens in one sample, 32 / 4
 // heads, 65 sums of 63 terms: 193 us with each address from the term before, 17 now).
 struct TailArgs {
     const float* partial;
     const int4* units;
     const int2* blk;
     int64_t n_main, T;
-    int n_tails, width, rows;   // rows: row blocks per chunk
+    int kt, n_tails, width, rows;   // rows: row blocks per chunk
     int hkv;
     float scale;
     __nv_bfloat16 *dk, *dv;
     const int* plan_status;
 };
-constexpr int kSumSplit = 8;        // blocks for a key block's 128 keys
+constexpr int kSumRows = 16;        // keys of a block
 template <int D>
-__global__ void __launch_bounds__(16 * D / 4) k_sum_tails(const TailArgs a) {
+__global__ void __launch_bounds__(kSumRows * D / 4) k_sum_tails(const TailArgs a) {
     grid_dep_wait();
     if (*a.plan_status != 0) return;
     const int idx = blockIdx.x, kvh = blockIdx.y >> 1, which = blockIdx.y & 1;
     const int4 first = a.units[a.n_main + idx];
     if (first.z == 0 || a.units[first.x].w != idx) return;
-    const int n = (a.blk[first.x].y - 1) / kBlk / a.rows - idx / a.width + 1;   // chunks up to the last that sees the block
-    const int r = blockIdx.z * (kBlk / kSumSplit) + threadIdx.x / (D / 4), col = threadIdx.x % (D / 4) * 4;
-    const size_t slot = (size_t)a.hkv * 2 * kBlk * D;
-    const float* p = a.partial + (((size_t)kvh * 2 + which) * kBlk + r) * D + col;
+    const int64_t k0 = (int64_t)first.x * a.kt;
+    int end = a.blk[k0 / kBlk].y;
+    if (a.kt > kBlk && k0 + kBlk < a.T) end = max(end, a.blk[k0 / kBlk + 1].y);
+    const int n = (end - 1) / kBlk / a.rows - idx / a.width + 1;   // chunks up to the last that sees the block
+    const int r = blockIdx.z * kSumRows + threadIdx.x / (D / 4), col = threadIdx.x % (D / 4) * 4;
+    const size_t slot = (size_t)a.hkv * 2 * a.kt * D;
+    const float* p = a.partial + (((size_t)kvh * 2 + which) * a.kt + r) * D + col;
     float4 sum = *reinterpret_cast<const float4*>(p + idx * slot);
     p += (size_t)(a.n_tails + idx) * slot;
     for (int i = 0; i < n; i += 8) {
@@ -815,13 +824,22 @@ __global__ void __launch_bounds__(16 * D / 4) k_sum_tails(const TailArgs a) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) { sum.x += v[k].x; sum.y += v[k].y; sum.z += v[k].z; sum.w += v[k].w; }
     }
-    const int64_t key = (int64_t)first.x * kBlk + r;
+    const int64_t key = k0 + r;
     if (key >= a.T) return;
     const float mul = which == 0 ? a.scale : 1.0f;
     uint2 w;
     w.x = pack_bf16x2(sum.x * mul, sum.y * mul);
     w.y = pack_bf16x2(sum.z * mul, sum.w * mul);
     *reinterpret_cast<uint2*>((which == 0 ? a.dk : a.dv) + ((size_t)key * a.hkv + kvh) * D + col) = w;
+}
+
+template <int D>
+static cudaError_t launch_sum_tails(const libra_plan_t* plan, const PlanDir& d, const float* partial, int hkv, float scale, void* dk,
+                                    void* dv, cudaStream_t s) {
+    const TailArgs a = {partial, d.d_units, plan->d_blk, d.NB - d.n_tails, plan->T, d.tile, d.n_tails, d.tail_width, d.tail_rows, hkv,
+                        scale, (__nv_bfloat16*)dk, (__nv_bfloat16*)dv, plan->d_status};
+    count_launch();
+    return launch_dependent(k_sum_tails<D>, dim3(d.n_tails, 2 * hkv, d.tile / kSumRows), kSumRows * D / 4, 0, s, a);
 }
 
 struct BwdWorkspace {
@@ -832,7 +850,7 @@ struct BwdWorkspace {
 };
 static BwdWorkspace bwd_workspace(int64_t T, int hq, int hkv, int d, bool fused, int n_tails) {
     BwdWorkspace w;
-    w.tail_bytes = fused || d == 256 ? 0 : (size_t)2 * n_tails * hkv * 2 * 128 * d * sizeof(float);
+    w.tail_bytes = fused ? 0 : (size_t)2 * n_tails * hkv * 2 * (d == 256 ? 256 : 128) * d * sizeof(float);
     w.Tpad = (T + 127) / 128 * 128;
     w.stat_bytes = ((size_t)hq * w.Tpad * sizeof(float) + 255) & ~(size_t)255;
     w.total = 2 * w.stat_bytes + w.tail_bytes;
@@ -847,7 +865,7 @@ static BwdWorkspace bwd_workspace(int64_t T, int hq, int hkv, int d, bool fused,
 // A plan with pair tiles selects the accumulating forms: at head_dim 128 the fused kernel (dQ, dK, dV accumulated in
 // fp32), at head_dim 256 the dV and dK passes over pair tiles (dK, dV accumulated in fp32; the dQ pass is unchanged).
 static bool use_fused(const libra_plan_t* plan, const libra_dims* dims) {
-    return plan->dir[2].enabled && (dims->head_dim == 128 || dims->head_dim == 256);
+    return plan->dir[2].enabled && ((dims->head_dim == 128 && !plan->two_kernel) || dims->head_dim == 256);
 }
 
 template <typename Kernel>
@@ -865,11 +883,13 @@ static int launch_bwd(const CUtensorMap& tq, const CUtensorMap& tk, const CUtens
         if (set_smem(k_attn_bwd_dkdv<D, false, false>, DkvSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
         if (set_smem(k_attn_bwd_dkdv<D, true, false>, DkvSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
         if (set_smem(k_attn_bwd_dkdv<D, false, true>, DkvSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
+        if (set_smem(k_attn_bwd_dkdv<D, true, true>, DkvSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
         if (set_smem(k_attn_bwd_dq<D, false>, DqSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
         if (set_smem(k_attn_bwd_dq<D, true>, DqSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
         if (!regs_pool_ok(k_attn_bwd_dkdv<D, false, false>, 128, kDkvRegsDs, 128, kDkvRegsOther)) return LIBRA_ERR_UNSUPPORTED;
         if (!regs_pool_ok(k_attn_bwd_dkdv<D, true, false>, 128, kDkvRegsDs, 128, kDkvRegsOther)) return LIBRA_ERR_UNSUPPORTED;
         if (!regs_pool_ok(k_attn_bwd_dkdv<D, false, true>, 128, kDkvRegsDs, 128, kDkvRegsOther)) return LIBRA_ERR_UNSUPPORTED;
+        if (!regs_pool_ok(k_attn_bwd_dkdv<D, true, true>, 128, kDkvRegsDs, 128, kDkvRegsOther)) return LIBRA_ERR_UNSUPPORTED;
         if (!regs_pool_ok(k_attn_bwd_dq<D, false>, 128 * kDqGroups, kDqRegsCompute, 128, kDqRegsOther)) return LIBRA_ERR_UNSUPPORTED;
         if (!regs_pool_ok(k_attn_bwd_dq<D, true>, 128 * kDqGroups, kDqRegsCompute, 128, kDqRegsOther)) return LIBRA_ERR_UNSUPPORTED;
         cfg_mark(kSlot);
@@ -880,14 +900,16 @@ static int launch_bwd(const CUtensorMap& tq, const CUtensorMap& tk, const CUtens
     const unsigned grid = Wa / share * share;
     mp->n_outcome[1] = (int)grid;
     mp->n_outcome[3] = Wb;
-    switch (share) {
-        case 8: e = launch_dependent<8>(k_attn_bwd_dkdv<D, true, false>, grid, kBwdThreads, bytes, s, tq, tk, tv, tdo, pa); break;
-        case 4: e = launch_dependent<4>(k_attn_bwd_dkdv<D, true, false>, grid, kBwdThreads, bytes, s, tq, tk, tv, tdo, pa); break;
-        case 2: e = launch_dependent<2>(k_attn_bwd_dkdv<D, true, false>, grid, kBwdThreads, bytes, s, tq, tk, tv, tdo, pa); break;
-        default:
-            if (pa.units) e = launch_dependent(k_attn_bwd_dkdv<D, false, true>, grid, kBwdThreads, bytes, s, tq, tk, tv, tdo, pa);
-            else e = launch_dependent(k_attn_bwd_dkdv<D, false, false>, grid, kBwdThreads, bytes, s, tq, tk, tv, tdo, pa);
-    }
+    auto launch = [&](auto shared, auto alone) {
+        switch (share) {
+            case 8: return launch_dependent<8>(shared, grid, kBwdThreads, bytes, s, tq, tk, tv, tdo, pa);
+            case 4: return launch_dependent<4>(shared, grid, kBwdThreads, bytes, s, tq, tk, tv, tdo, pa);
+            case 2: return launch_dependent<2>(shared, grid, kBwdThreads, bytes, s, tq, tk, tv, tdo, pa);
+            default: return launch_dependent(alone, grid, kBwdThreads, bytes, s, tq, tk, tv, tdo, pa);
+        }
+    };
+    e = pa.units ? launch(k_attn_bwd_dkdv<D, true, true>, k_attn_bwd_dkdv<D, false, true>)
+                 : launch(k_attn_bwd_dkdv<D, true, false>, k_attn_bwd_dkdv<D, false, false>);
     time_end(mp, 1, s);
     time_begin(mp, 2, s);
     if (e == cudaSuccess)
@@ -896,13 +918,9 @@ static int launch_bwd(const CUtensorMap& tq, const CUtensorMap& tk, const CUtens
     time_end(mp, 2, s);
     count_launch(2);
     if (pa.units && e == cudaSuccess) {
-        const PlanDir& d = mp->dir[5];
         time_begin(mp, 5, s);
-        const TailArgs ta = {pa.partial, pa.units, pa.blk, d.NB - d.n_tails, pa.T, d.n_tails, d.tail_width, d.tail_rows, pa.hkv,
-                             pa.scale, pa.dk, pa.dv, pa.plan_status};
-        e = launch_dependent(k_sum_tails<D>, dim3(d.n_tails, 2 * pa.hkv, kSumSplit), 16 * D / 4, 0, s, ta);
+        e = launch_sum_tails<D>(mp, mp->dir[5], pa.partial, pa.hkv, pa.scale, pa.dk, pa.dv, s);
         time_end(mp, 5, s);
-        count_launch();
     }
     return e == cudaSuccess ? LIBRA_OK : LIBRA_ERR_CUDA;
 }
@@ -947,7 +965,7 @@ extern "C" size_t libra_attn_pool_bwd_workspace_bytes(const libra_plan_t* plan, 
     if (!plan || !dims || dims->hq <= 0 || dims->hkv <= 0 ||
         (dims->head_dim != 64 && dims->head_dim != 128 && dims->head_dim != 256))
         return 0;
-    return bwd_workspace(plan->T, dims->hq, dims->hkv, dims->head_dim, use_fused(plan, dims), plan->dir[5].n_tails).total;
+    return bwd_workspace(plan->T, dims->hq, dims->hkv, dims->head_dim, use_fused(plan, dims), plan->dir[dims->head_dim == 256 ? 6 : 5].n_tails).total;
 }
 
 // fp32 tensor [T, H, 128] viewed as (128, H, T); box = 32 floats x 1 head x 32 rows, 128-byte swizzle.
@@ -1096,7 +1114,7 @@ static int backward(const void* q_dev, const void* k_dev, const void* v_dev, Row
 
     const int D = dims->head_dim;
     const int64_t T = plan->T;
-    const BwdWorkspace ws = bwd_workspace(T, dims->hq, dims->hkv, D, fused, plan->dir[5].n_tails);
+    const BwdWorkspace ws = bwd_workspace(T, dims->hq, dims->hkv, D, fused, plan->dir[D == 256 ? 6 : 5].n_tails);
     float* dvec = reinterpret_cast<float*>(workspace_dev);
     float* lse2 = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace_dev) + ws.stat_bytes);
     cudaStream_t s = (cudaStream_t)stream;
@@ -1125,8 +1143,14 @@ static int backward(const void* q_dev, const void* k_dev, const void* v_dev, Row
         time_end(mp256, 3, s);
         if (e256 != cudaSuccess) return LIBRA_ERR_CUDA;
         mp256->bwd_mask = 2 | 4 | 8;
+        float* partial = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace_dev) + 2 * ws.stat_bytes);
         int rc256 = launch_bwd_d256(q_dev, k_dev, v_dev, dout_dev, dq_dev, dk_dev, dv_dev, lse2, dvec, ws.Tpad, dk_acc,
-                                    dv_acc, plan, dims, scale, s);
+                                    dv_acc, partial, plan, dims, scale, s);
+        if (rc256 == LIBRA_OK && !fused && plan->dir[6].enabled) {
+            time_begin(mp256, 5, s);
+            if (launch_sum_tails<256>(plan, plan->dir[6], partial, dims->hkv, scale, dk_dev, dv_dev, s) != cudaSuccess) rc256 = LIBRA_ERR_CUDA;
+            time_end(mp256, 5, s);
+        }
         if (rc256 == LIBRA_OK && fused) {
             time_begin(mp256, 5, s);
             const int64_t nk8 = T * dims->hkv * 256 / 8;
@@ -1209,8 +1233,9 @@ static int backward(const void* q_dev, const void* k_dev, const void* v_dev, Row
     int64_t reach = T / plan->n;   // rows that see a key block, on average
     if (plan->window && reach > plan->window + kBlk) reach = plan->window + kBlk;
     const int64_t its = (int64_t)(dims->hq / dims->hkv) * reach / kBlk;
-    int share = dims->hq > dims->hkv && !pa.units ? 8 : 1;
-    while (share > 1 && (share * dkv_dir.NT > dkv_dir.W || 2 * share > its)) share /= 2;
+    // (Empty tiles of lists with tails share a worker behind the others.)
+    int share = dims->hq > dims->hkv ? 8 : 1;
+    while (share > 1 && (share * dkv_lists.NT > dkv_dir.W || 2 * share > its)) share /= 2;
     libra_plan_t* mp = const_cast<libra_plan_t*>(plan);
     return D == 128 ? launch_bwd<128>(tq, tk, tv, tdo, tdq, pa, dkv_dir.W, share, pb, dq_dir.W, mp, s)
                     : launch_bwd<64>(tq, tk, tv, tdo, tdq, pa, dkv_dir.W, share, pb, dq_dir.W, mp, s);

@@ -117,6 +117,10 @@ struct Params {
     const int32_t* u_chunk; // [NU] query chunk of pair-block u
     int64_t NU;
     int R;                  // 128-row blocks per query chunk
+    // key-stationary passes of plans with sinks over key-major tiles (SINK): key block, first row block, row blocks, slot of partial
+    // sums (k_tail_units in plan.cu)
+    const int4* units;
+    float* partial;         // [slots][Hkv][dK, dV][256][256]
     float scale, scale_log2;
     int* outcome;
     int side_by_side;       // DK, DQ: start without waiting for the pass ahead
@@ -128,7 +132,8 @@ struct Params {
 
 // Walks the units of a CTA pair in the order every role of both CTAs uses.
 //   key-stationary passes: one unit per tile of the pair's list (256 keys x one kv head); its iterations are the query
-//   heads of the group times the 64-row query blocks from the diagonal to the end of the last key's sample (of the chunk);
+//   heads of the group times the 64-row query blocks from the diagonal to the end of the last key's sample (of the chunk; SINK: of
+//   the unit);
 //   query-stationary passes: a query-major tile (256 rows x head shard) of the lists of two workers gives one unit per
 //   head; its iterations are the 64-key blocks from the first key that the first row's window holds to the diagonal.  SINK:
 //   ahead of them the blocks below that hold the sinks of the first row's sample.
@@ -141,7 +146,8 @@ struct Units {
     int64_t base, r0;       // first stationary row of the pair and of this CTA
     int h, kvh, b_lo, n_blk, n_it;
     int bound0, bound1;     // of each CTA's rows: first key that the first one's window holds (queries), end of the queries that see one (keys)
-    int early, early_lo;    // SINK: blocks ahead of the window's, the first of them
+    int early, early_lo;    // SINK, queries: blocks ahead of the window's, the first of them
+    int slot;               // SINK, keys: where the partial sums go, -1: the results are stored
     __device__ Units(const Params& p_, int cta) : p(p_) {
         const int c = cta >> 1;
         if (kKeys) {
@@ -158,8 +164,23 @@ struct Units {
     }
     __device__ bool next(uint32_t rank) {
         if (++hh == hps) { hh = 0; if (++idx >= end) return false; }
+        if constexpr (kKeys && SINK)
+            while (p.units[p.cta_tiles[idx] / p.hkv].z == 0)   // an empty one
+                if (++idx >= end) return false;
         const int t = p.cta_tiles[idx];
-        if constexpr (kKeys) {
+        if constexpr (kKeys && SINK) {
+            const int4 u = p.units[t / p.hkv];
+            kvh = t % p.hkv;
+            base = (int64_t)u.x * (2 * kRows);
+            bound0 = p.blk[base / kRows].y;
+            bound1 = base + kRows < p.T ? p.blk[base / kRows + 1].y : bound0;
+            const int last64 = ((bound1 > bound0 ? bound1 : bound0) - 1) / kBlk, hi64 = 2 * (u.y + u.z) - 1;
+            b_lo = 2 * u.y;
+            n_blk = (hi64 < last64 ? hi64 : last64) - b_lo + 1;
+            slot = u.w;
+            h = kvh * G;
+            n_it = G * n_blk;
+        } else if constexpr (kKeys) {
             const int j = p.acc32 ? p.u_blk[(int)(t % p.NU)] : t / p.hkv;
             kvh = p.acc32 ? (int)(t / p.NU) : t % p.hkv;
             base = (int64_t)j * (2 * kRows);
@@ -220,7 +241,7 @@ struct Units {
         lo = kKeys ? (int)(a / kBlk) : bound / kBlk;
         hi = kKeys ? (bound - 1) / kBlk : (int)(z / kBlk);
         lo = lo > b_lo ? lo - b_lo : 0;
-        if constexpr (SINK) {
+        if constexpr (SINK && !kKeys) {
             lo += early;
             hi += early;
         }
@@ -228,7 +249,7 @@ struct Units {
     }
     // First row of the streamed block j of a head; the iterations of a unit take its heads in turn, blocks ascending.
     __device__ int stream_row(int j) const {
-        if constexpr (SINK) return (j < early ? early_lo + j : b_lo + j - early) * kBlk;
+        if constexpr (SINK && !kKeys) return (j < early ? early_lo + j : b_lo + j - early) * kBlk;
         return (b_lo + j) * kBlk;
     }
 };
@@ -432,7 +453,7 @@ k_attn_d256(const __grid_constant__ CUtensorMap tm_sa, const __grid_constant__ C
                 u.seen_by(0, lo0, hi0);
                 u.seen_by(1, lo1, hi1);
                 int elo0 = 0, ehi0 = -1, elo1 = 0, ehi1 = -1;
-                if constexpr (SINK) {
+                if constexpr (SINK && !L::kKeyStationary) {
                     u.early_by(0, elo0, ehi0);
                     u.early_by(1, elo1, ehi1);
                 }
@@ -517,7 +538,7 @@ k_attn_d256(const __grid_constant__ CUtensorMap tm_sa, const __grid_constant__ C
                 hi_abs = row_ok ? (int)row : -1;
             }
             int sink_lo = 0, sink_hi = -1;           // SINK: the row's sinks ahead of its window
-            if (SINK && row_ok) {
+            if (SINK && !L::kKeyStationary && row_ok) {
                 sink_lo = p.tok_first[row] - col0;
                 sink_hi = (int)min((int64_t)p.tok_first[row] + p.sinks, (int64_t)p.tok_start[row]) - 1 - col0;
             }
@@ -635,7 +656,7 @@ k_attn_d256(const __grid_constant__ CUtensorMap tm_sa, const __grid_constant__ C
                     if (need_mask) {
                         static_assert(MODE == FWD || NC == 32, "one mask word per compute thread");
                         uint32_t vis = range_bits(c_lo, c_hi);
-                        if (SINK) vis |= range_bits(sink_lo - b0, sink_hi - b0);
+                        if (SINK && !L::kKeyStationary) vis |= range_bits(sink_lo - b0, sink_hi - b0);
 #pragma unroll
                         for (int i = 0; i < NC; ++i) pf[i] = (vis >> i) & 1u ? pf[i] : 0.f;
                     }
@@ -706,6 +727,16 @@ k_attn_d256(const __grid_constant__ CUtensorMap tm_sa, const __grid_constant__ C
                 u.seen_by(rank, lo, hi);
                 row_ok = row_ok && lo <= hi;
             }
+            float* part_row = nullptr;
+            bool none = false;
+            if constexpr (SINK && L::kKeyStationary)
+                if (u.slot >= 0) {
+                    int lo, hi;
+                    u.seen_by(rank, lo, hi);
+                    none = lo > hi;                  // of the unit's blocks this CTA's keys have seen none: its accumulator was not begun
+                    part_row = p.partial + ((((size_t)u.slot * p.hkv + u.kvh) * 2 + (MODE == DV)) * 2 * kRows + rank * kRows + r) * kD +
+                               grp * (kD / L::kGroups);
+                }
             float* acc_row = L::kKeyStationary && p.acc32
                                  ? p.acc32 + ((size_t)row * n_heads + head) * kD + grp * (kD / L::kGroups) : nullptr;
 #pragma unroll
@@ -713,7 +744,12 @@ k_attn_d256(const __grid_constant__ CUtensorMap tm_sa, const __grid_constant__ C
                 uint32_t v[32];
                 tmem_ld32(t_acc + c, v);
                 tmem_ld_wait();
-                if (acc_row) {   // a key block meets several query chunks: its partial sums are added up in fp32
+                if (part_row) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4)
+                        *reinterpret_cast<uint4*>(part_row + c + i) =
+                            none ? make_uint4(0, 0, 0, 0) : make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                } else if (acc_row) {   // a key block meets several query chunks: its partial sums are added up in fp32
                     if (row_ok) {
 #pragma unroll
                         for (int i = 0; i < 32; i += 4)
@@ -883,12 +919,13 @@ int launch_fwd_d256(const void* q, const void* k, const void* v, void* out, floa
 // Backward at head_dim 256: the dV and dK passes over the key-major lists, the dQ pass over the query-major lists.
 // lse2 / dvec are the row statistics [Hq, Tpad] the caller has computed on the same stream.
 int launch_bwd_d256(const void* q, const void* k, const void* v, const void* dout, void* dq, void* dk, void* dv,
-                    const float* lse2, const float* dvec, int64_t Tpad, float* dk_acc, float* dv_acc,
+                    const float* lse2, const float* dvec, int64_t Tpad, float* dk_acc, float* dv_acc, float* partial,
                     const libra_plan* plan, const libra_dims* dims, float scale, cudaStream_t s) {
     using namespace d256;
     const PlanDir& dq_dir = plan->dir[0];
     const bool pairs = dk_acc != nullptr;            // key-stationary passes over pair tiles, fp32 accumulators
-    const PlanDir& kv_dir = plan->dir[3];            // 256 keys a tile, in pair tiles or key-major
+    const bool tails = !pairs && plan->dir[6].enabled;
+    const PlanDir& kv_dir = plan->dir[tails ? 6 : 3];   // 256 keys a tile, in pair tiles or key-major
     if (!kv_dir.enabled || (kv_dir.d_u_blk != nullptr) != pairs) return LIBRA_ERR_PLAN_MISMATCH;
     // whole 128-row tiles (stationary), halves of a streamed block's rows (32) and of its columns (64-row boxes)
     CUtensorMap q128, do128, k128, v128, q32, do32, k32, v32, q64, do64, k64;
@@ -924,13 +961,18 @@ int launch_bwd_d256(const void* q, const void* k, const void* v, const void* dou
     time_begin(mp, 1, s);
     prm.out = reinterpret_cast<__nv_bfloat16*>(dv);
     prm.acc32 = dv_acc;
-    rc = launch<DV, false>(k128, k128, q32, do64, do64, prm, plan->W, mp, s);
+    prm.units = kv_dir.d_units;
+    prm.partial = partial;
+    rc = tails ? launch<DV, true>(k128, k128, q32, do64, do64, prm, plan->W, mp, s)
+               : launch<DV, false>(k128, k128, q32, do64, do64, prm, plan->W, mp, s);
     prm.out = reinterpret_cast<__nv_bfloat16*>(dk);
     prm.acc32 = dk_acc;
     prm.outcome = plan->d_outcome[2];
     prm.side_by_side = side_by_side(kv_dir.NT, kv_dir.W);
     prm.busy = plan->dir[pairs ? 2 : 1].d_busy;
-    if (rc == LIBRA_OK) rc = launch<DK, false>(k128, v128, q32, do32, q64, prm, plan->W, mp, s);
+    if (rc == LIBRA_OK)
+        rc = tails ? launch<DK, true>(k128, v128, q32, do32, q64, prm, plan->W, mp, s)
+                   : launch<DK, false>(k128, v128, q32, do32, q64, prm, plan->W, mp, s);
     time_end(mp, 1, s);
     prm.acc32 = nullptr;
     if (rc != LIBRA_OK) return rc;

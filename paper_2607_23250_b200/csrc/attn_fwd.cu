@@ -254,6 +254,79 @@ __device__ __noinline__ bool exchange_partial(uint8_t* smem, uint64_t* bars, uin
     return true;
 }
 
+// SINK: a block ahead of the slot's window, whose groups of 32 columns at.x .. at.y hold sinks; those at columns at.z .. at.w are
+// visible to the row.  ml: the row's reference maximum and sum so far, returned with the block's; a negative sum on a timeout.
+// A group is read twice, for the maximum and for the exponentials.  (A function of its own, to keep its registers out of the loop over the
+// window's blocks.  All 128 columns of such a block, as of the others: 4096 tokens, 4 heads of 64, window 512: 17.0 us, inlined
+// 16.4, so 16.3; step of 131072 tokens, 32 / 8 heads, window 1024: 11.0 and 10.7 ms.)
+template <int D>
+__device__ __noinline__ float2 sink_block(uint8_t* smem, uint64_t* bars, uint32_t t_s, uint32_t t_o, int4 at, float scale_log2, float2 ml,
+                                          uint32_t s_parity, uint32_t o_parity) {
+    using L = FwdSmem<D>;
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::kMiscOff + 4);
+    const int g = threadIdx.x >> 7;
+    uint64_t* q = bars + 2 * L::kStages;   // (see the kernel)
+    const float2 gave_up = make_float2(0.f, -1.f);
+    if (!warp_wait(q + 2 + g, s_parity, abort_flag)) return gave_up;
+    tc_fence_after();
+    float mx = -INFINITY;
+#pragma unroll 1
+    for (int c = at.x; c <= at.y; ++c) {
+        uint32_t s[32];
+        tmem_ld32(t_s + 32 * c, s);
+        tmem_ld_wait();
+        const uint32_t vis = range_bits(at.z - 32 * c, at.w - 32 * c);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) mx = fmaxf(mx, (vis >> i) & 1u ? __uint_as_float(s[i]) : -INFINITY);
+    }
+    mx *= scale_log2;
+    float factor = 1.0f;
+    if (mx > ml.x + kRescaleThreshold) {
+        factor = ex2_approx(ml.x - mx);
+        ml.x = mx;
+    }
+    if (__any_sync(0xffffffffu, factor != 1.0f)) {
+        if (!warp_wait(q + 6 + g, o_parity, abort_flag)) return gave_up;
+        tc_fence_after();
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+            uint32_t o[32];
+            tmem_ld32(t_o + c, o);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * factor);
+            tmem_st32(t_o + c, o);
+        }
+        tmem_st_wait();
+    }
+    ml.y *= factor;
+    const float m_use = ml.x == -INFINITY ? 0.f : ml.x;
+    // (P of group c lies over S of group c / 2, which has been read)
+#pragma unroll 1
+    for (int c = at.x; c <= at.y; ++c) {
+        uint32_t s[32], pk[16];
+        tmem_ld32(t_s + 32 * c, s);
+        tmem_ld_wait();
+        const uint32_t vis = range_bits(at.z - 32 * c, at.w - 32 * c);
+        float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+            const float p0 = (vis >> i) & 1u ? ex2_approx(fmaf(__uint_as_float(s[i]), scale_log2, -m_use)) : 0.f;
+            const float p1 = (vis >> (i + 1)) & 1u ? ex2_approx(fmaf(__uint_as_float(s[i + 1]), scale_log2, -m_use)) : 0.f;
+            sum0 += p0;
+            sum1 += p1;
+            pk[i >> 1] = pack_bf16x2(p0, p1);
+        }
+        ml.y += sum0 + sum1;
+        tmem_st16(t_s + 16 * c, pk);
+    }
+    tmem_st_wait();
+    tc_fence_before();
+    mbar_arrive(q + 8 + g);
+    mbar_arrive(q + 4 + g);
+    return ml;
+}
+
 // PAIR: a cluster of two CTAs goes through the list of a worker of its own and shares its tiles by key blocks.  When there
 // is no more than a tile for every two SMs, the longest tile is the launch: 16 of its key blocks take 26 us (4096 tokens, 4
 // heads of 64), at the rate of one slot's chain for each, with 84 SMs idle.  Each rank takes
@@ -644,61 +717,18 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
                     mbar_arrive(&bar_pready[g]);
                     ++ocnt;
                 }
-                if constexpr (SINK) {   // the same for the blocks of sinks, a group of 32 columns at a time
+                if constexpr (SINK) {   // the same for the blocks of sinks
                     for (int j = x.shi[g]; j >= x.slo[g] && ok; --j) {
-                        ok = warp_wait(&bar_sfull[g], scnt & 1, abort_flag);
-                        if (!ok) break;
-                        ++scnt;
-                        tc_fence_after();
                         int c0, c1;
                         x.sink_groups(g, j, p.sinks, c0, c1);
-                        const int s_lo = sink_lo - j * kBN, s_hi = sink_hi - j * kBN;
-                        float mx = -INFINITY;
-#pragma unroll 1
-                        for (int c = c0; c <= c1; ++c) {
-                            uint32_t s[32];
-                            tmem_ld32(t_s + 32 * c, s);
-                            tmem_ld_wait();
-                            const uint32_t vis = range_bits(s_lo - 32 * c, s_hi - 32 * c);
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) mx = fmaxf(mx, (vis >> i) & 1u ? __uint_as_float(s[i]) : -INFINITY);
-                        }
-                        mx *= p.scale_log2;
-                        float factor = 1.0f;
-                        if (mx > m_ref + kRescaleThreshold) {
-                            factor = ex2_approx(m_ref - mx);
-                            m_ref = mx;
-                        }
-                        if (__any_sync(0xffffffffu, factor != 1.0f)) {
-                            ok = rescale_o(factor);
-                            if (!ok) break;
-                        }
-                        l_sum *= factor;
-                        const float m_use = (m_ref == -INFINITY) ? 0.f : m_ref;
-                        // (P of group c lies over S of group c / 2, which has been read)
-#pragma unroll 1
-                        for (int c = c0; c <= c1; ++c) {
-                            uint32_t s[32], pk[16];
-                            tmem_ld32(t_s + 32 * c, s);
-                            tmem_ld_wait();
-                            const uint32_t vis = range_bits(s_lo - 32 * c, s_hi - 32 * c);
-                            float sum0 = 0.f, sum1 = 0.f;
-#pragma unroll
-                            for (int i = 0; i < 32; i += 2) {
-                                const float p0 = (vis >> i) & 1u ? ex2_approx(fmaf(__uint_as_float(s[i]), p.scale_log2, -m_use)) : 0.f;
-                                const float p1 = (vis >> (i + 1)) & 1u ? ex2_approx(fmaf(__uint_as_float(s[i + 1]), p.scale_log2, -m_use)) : 0.f;
-                                sum0 += p0;
-                                sum1 += p1;
-                                pk[i >> 1] = pack_bf16x2(p0, p1);
-                            }
-                            l_sum += sum0 + sum1;
-                            tmem_st16(t_s + 16 * c, pk);
-                        }
-                        tmem_st_wait();
-                        tc_fence_before();
-                        mbar_arrive(&bar_ppart[g]);
-                        mbar_arrive(&bar_pready[g]);
+                        const float2 ml = sink_block<D>(smem, bars, t_s, t_o, make_int4(c0, c1, sink_lo - j * kBN, sink_hi - j * kBN), p.scale_log2,
+                                                        make_float2(m_ref, l_sum), scnt & 1, (ocnt - 1) & 1);
+                        ok = __all_sync(0xffffffffu, ml.y >= 0.f);
+                        if (!ok) break;
+                        ++scnt;
                         ++ocnt;
+                        m_ref = ml.x;
+                        l_sum = ml.y;
                     }
                 }
                 if (!ok) break;

@@ -38,7 +38,7 @@ struct PlanDir {
     // plans with sinks: the key blocks ahead of first_j that rows of the chunk see all the same (pair-blocks base .. base + n - 1)
     int32_t* d_sink_j = nullptr;       // [chunks] first of them
     int32_t* d_sink_n = nullptr;       // [chunks] their number
-    // key-major tiles with the sinks' tails apart (direction 5): key block, first row block, row blocks, slot of partial sums
+    // key-major tiles with the sinks' tails apart (directions 5 and 6): key block, first row block, row blocks, slot of partial sums
     int4* d_units = nullptr;           // [NB]
     int n_tails = 0, tail_width = 0, tail_rows = 0;   // the last n_tails units, tail_width of them for each chunk of tail_rows row blocks
 };
@@ -69,12 +69,15 @@ struct libra_plan {
     int* d_outcome[4] = {};          // [W + 1] each: kernels on pairs of CTAs round the workers up to even
     int n_outcome[4] = {};           // CTAs of that launch: clusters leave the last workers out, pairs may add one
     int W = 0;                       // workers of every direction
+    int asked = 0;                   // directions the caller asked for (key-major lists may be there for the library's own use)
+    int two_kernel = 0;              // pair tiles or not, the backward at head_dim 128 takes the two-kernel form (prefer_two_kernels)
     int bwd_mask = 0;                // which of d_outcome[1..3] the last backward wrote
     // 0 = query-major, 1 = key-major, 2 = pair tiles (key block x query chunk), 3 = the key-stationary tiles of kernels that
     // run on pairs of CTAs: as 2 when that is there, else as 1, with 256 keys a tile and a worker for every two; 4 = the pair
     // tiles of the fused kernel on pairs of CTAs, 256 keys a tile and the query chunks of 2; 5 = as 1 with a window and sinks:
-    // what a key block that holds sinks is seen by beyond its window is cut into tiles of their own
-    static constexpr int kDirs = 6;
+    // what a key block that holds sinks is seen by beyond its window is cut into tiles of their own; 6 = the same for 3, where
+    // that is not made of pair tiles
+    static constexpr int kDirs = 7;
     libra::PlanDir dir[kDirs];
     uint32_t wait_limit_ns = 2000000000u;  // budget of one device-side wait (libra_plan_set_wait_limit_ns)
     int inject_stall = 0;            // test aid: the producer role issues no loads (libra_plan_inject_stall)
@@ -125,8 +128,9 @@ int launch_fwd_d256(const void* q, const void* k, const void* v, void* out, floa
                     const libra_dims* dims, float scale, cudaStream_t s);
 // dk_acc / dv_acc: fp32 accumulators [T, Hkv, 256], zero on entry, when the dV and dK passes are to walk the plan's
 // pair tiles (the caller rounds them afterwards); null: key-major tiles, dk / dv written directly.
+// partial: slots of partial sums, for plans with direction 6 (the caller adds them up).
 int launch_bwd_d256(const void* q, const void* k, const void* v, const void* dout, void* dq, void* dk, void* dv,
-                    const float* lse2, const float* dvec, int64_t Tpad, float* dk_acc, float* dv_acc,
+                    const float* lse2, const float* dvec, int64_t Tpad, float* dk_acc, float* dv_acc, float* partial,
                     const libra_plan* plan, const libra_dims* dims, float scale, cudaStream_t s);
 }  // namespace libra
 

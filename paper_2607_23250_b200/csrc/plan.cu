@@ -212,7 +212,7 @@ __global__ void k_block_weights(const MaskView m, const DirViews views) {
     if (lane == 0) d.weight_blk[b] = w;
 }
 
-// Key-major tiles of plans with sinks (direction 5; the two-kernel backward).  A key block that holds sinks of a long sample is
+// Key-major tiles of plans with sinks (directions 5 and 6, key blocks of kt = 128 and 256; the two-kernel backward).  A key block that holds sinks of a long sample is
 // seen by all of it: one tile a block, as the exported lists have it, made that tile the launch (16000 tokens in one sample, 8 / 2
 // heads of 64, window 1001: 500 row blocks of the 68 that a CTA has on average, 899 us).  So of such a block the row blocks up to the
 // end of the chunk of R in which its window ends are the main tile, and those of each later chunk are a tile of their own.
@@ -221,25 +221,33 @@ __global__ void k_block_weights(const MaskView m, const DirViews views) {
 // there are fewer.  The partial sums of main tile and tails have slots of their own (w; -1: none, the results are stored) and are added up
 // in the order of the chunks, so that the result does not depend on the schedule.
 __global__ void k_tail_units(const MaskView m, const int2* __restrict__ blk, const int32_t* __restrict__ blk_near,
-                             int64_t n_main, int R, int width, const DirView d) {
+                             int64_t n_main, int kt, int R, int width, const DirView d) {
     const int64_t u = blockIdx.x * (int64_t)blockDim.x + threadIdx.x;
     if (u >= d.NB) return;
     const int n_tails = (int)(d.NB - n_main);
+    const int B = kt / 128, last_blk = (int)((m.T - 1) / 128);
+    // of key block j: row block of the last query that sees one of its keys, the same by their windows alone
+    auto last_of = [&](int j) {
+        int e = blk[j * B].y;
+        if (B == 2 && 2 * j + 1 <= last_blk && blk[2 * j + 1].y > e) e = blk[2 * j + 1].y;
+        return (e - 1) / 128;
+    };
+    auto near_of = [&](int j) { return (blk_near[j * B + B - 1 < last_blk ? j * B + B - 1 : last_blk] - 1) / 128; };
     int4 unit = make_int4(0, 0, 0, -1);
     if (u < n_main) {
-        const int j = (int)u, last = (blk[j].y - 1) / 128, c = (blk_near[j] - 1) / 128 / R;
+        const int j = (int)u, last = last_of(j), c = near_of(j) / R;
         const int end = last < c * R + R - 1 ? last : c * R + R - 1;
-        unit = make_int4(j, j, end - j + 1, -1);
+        unit = make_int4(j, j * B, end - j * B + 1, -1);
         if (last > end) {   // the first tail's number names the slot
-            const int x = j - m.tok_first[(int64_t)(c + 1) * R * 128] / 128;
+            const int x = j - m.tok_first[(int64_t)(c + 1) * R * 128] / kt;
             unit.w = x >= 0 && x < width ? (c + 1) * width + x : -1;   // (out of range: a malformed cu_seqlens, nothing will run)
         }
     } else {
         const int idx = (int)(u - n_main), c = idx / width;
-        const int64_t t0 = (int64_t)c * R * 128, a = m.tok_first[t0], j = a / 128 + idx % width;
+        const int64_t t0 = (int64_t)c * R * 128, a = m.tok_first[t0], j = a / kt + idx % width;
         const int64_t e = a + m.sinks < t0 ? a + m.sinks : t0;
-        if (j * 128 < e && (blk_near[j] - 1) / 128 / R < c) {
-            const int last = (blk[j].y - 1) / 128, end = last < c * R + R - 1 ? last : c * R + R - 1;
+        if (j * kt < e && near_of((int)j) / R < c) {
+            const int last = last_of((int)j), end = last < c * R + R - 1 ? last : c * R + R - 1;
             unit = make_int4((int)j, c * R, end - c * R + 1, n_tails + idx);
         }
     }
@@ -668,11 +676,25 @@ static bool fused_on_pairs(const libra_plan* p, int64_t cells, int64_t wide_cell
     if (cost >= 1.0) return false;
     return !own_choice || (R > 1 && wide_tiles * p->dir[4].H >= 2.4 * p->dir[4].W);
 }
+// Whether a windowed plan's backward takes the two-kernel form although it has pair tiles; `cells`: live 128 x 128 cells of a head.
+// The fused form's passes over memory (accumulators cleared, added to, rounded) cost the same however short the window, and
+// its tiles, a window long at most, start and end more often: on single CTAs it pays where a row block has many cells, or the
+// key-major tiles are few for the workers; with sinks fewer, since their tails need a pass more.  Backward, fused / two-kernel in us,
+// 131072 tokens, 32 / 8 heads, log-normal, window 128 (2 cells a row block): 4870 / 3500, 512: 6100 / 5600, 1024 (8): 8350 / 8000; 33001
+// tokens, 2048 (13): 2990 / 3180; 32768 tokens in one sample, 8 / 2 heads, 512: 490 / 383; 10007 in samples of up to 400, 8 / 2
+// heads, 128, a sink: 87 / 96 (158 key-major tiles, 148 workers), 17873 tokens, 4 / 1 heads, 79, none: 71 / 56 (140); 4133 tokens, 4 / 1 heads,
+// 802: 28 / 50 (33).  On pairs of CTAs: 65536 tokens, 32 / 4 heads, 4096: 11900 / 13800, 8192: 20900 / 24800.  On 160 pools of
+// 700 to 131072 tokens with windows of 32 to 8192 the choice is 1.2 % from the better form on average, always the fused
+// one 12 %, always the other 10 %.
+static bool prefer_two_kernels(const libra_plan* p, bool on_pairs, int64_t cells) {
+    if (!p->window || on_pairs || !p->dir[0].enabled || !p->dir[1].enabled) return false;
+    return cells <= 8 * p->dir[1].NB && 100 * p->dir[1].NT >= (p->sinks ? 135 : 90) * p->W;
+}
 static double heads_per_kv(const libra_plan* p) { return p->dir[0].H > p->dir[2].H ? (double)p->dir[0].H / p->dir[2].H : 1.0; }
 // Counts, choice and, while every size has more than 262144 pair-blocks, twice the largest.  `pairs`: whether the fused kernel's
 // wide tiles are under consideration, and whether they were taken.
 static int count_pair_blocks(libra_plan* p, const MaskView& mask, PairCands& cands, int64_t* d_totals, PairTables (&chosen)[libra_plan::kDirs], double G,
-                             bool own_choice, bool& pairs) {
+                             bool own_choice, bool& pairs, int64_t& cells) {
     const int dirs = cands.n_longest;
     for (;;) {
         int64_t totals[kPairTotals];
@@ -706,6 +728,7 @@ static int count_pair_blocks(libra_plan* p, const MaskView& mask, PairCands& can
                 p->dir[4].chunk = p->dir[2].chunk;
                 chosen[4] = cands.c[x];
             }
+        cells = totals[kPairCands + 2];
         if (pairs) pairs = fused_on_pairs(p, totals[kPairCands + 2], totals[kPairCands + 3], p->dir[4].NB, chosen[2].R, own_choice);
         return LIBRA_OK;
     }
@@ -724,23 +747,27 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
     const int64_t T = p->T;
     cudaStream_t s = p->stream;
     const bool wide_pairs = want[3] && want[2];                   // the wide tiles are pair tiles
-    const bool sorted[kDirs] = {want[0], want[1], false, want[3] && !want[2], false, want[5]};   // sizes known, placed heaviest first
-    bool pairs[kDirs] = {false, false, want[2], wide_pairs, want[4], false};
+    const bool sorted[kDirs] = {want[0], want[1], false, want[3] && !want[2], false, want[5], want[6]};   // sizes known, placed heaviest first
+    bool pairs[kDirs] = {false, false, want[2], wide_pairs, want[4], false, false};
     for (int k = 0; k < kDirs; ++k) {
         if (!sorted[k]) continue;
         p->dir[k].NB = (T + p->dir[k].tile - 1) / p->dir[k].tile;
-        if (k == 5) {
-            // Chunks of about half a window: a tail then weighs no more than other tiles.  Not so many of them that the slots of
-            // partial sums, 2 x 64 KB a tail and kv head at head_dim 64, are more than a few hundred.
+        if (k >= 5) {
+            // Chunks of about half a window, 8 row blocks at least, or what a worker has of them on average where that is less: a
+            // tail then weighs no more than other tiles, and no tile is the launch (4200 tokens, 4 / 1 heads, window 128, 64 sinks:
+            // backward 68.7 us with 8 row blocks a chunk at least, 44.7 so and with tiles shared by clusters).  Not so many chunks that the slots of partial sums, 2 x 64 KB a tail and kv head
+            // at head_dim 64, are more than a few hundred.
             PlanDir& d = p->dir[k];
-            const int64_t width = (p->sinks + 126) / 128 + 1, rows = (p->window / 128 + 1) / 2;
+            const int64_t kt = d.tile, width = (p->sinks + kt - 2) / kt + 1, rows = (p->window / 128 + 1) / 2;
+            const int64_t NRB = (T + 127) / 128, load = NRB * d.H * (p->window / 128 + 2) / p->W + 2;
             int64_t R = rows > 8 ? rows : 8;
+            R = R < load ? R : load;
             R = R > width ? R : width;
-            const int64_t least = width < 4 ? (d.NB + 63) / 64 : (d.NB * width + 255) / 256;
+            const int64_t least = width < 4 ? (NRB + 63) / 64 : (NRB * width + 255) / 256;
             R = R > least ? R : least;
             d.tail_rows = (int)R;
             d.tail_width = (int)width;
-            d.n_tails = (int)((d.NB + R - 1) / R * width);
+            d.n_tails = (int)((NRB + R - 1) / R * width);
             d.NB += d.n_tails;
         }
         if (const int rc = check_dir(p, p->dir[k], false); rc != LIBRA_OK) return rc;
@@ -748,6 +775,7 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
     PairCands cands;
     PairTables chosen[kDirs];
     int64_t* d_totals = nullptr;
+    int64_t cells = 0;
     if (want[2]) {
         if (p->dir[2].chunk % p->dir[2].tile) return LIBRA_ERR_INVALID_ARG;
         cands.rt = p->dir[2].tile;
@@ -796,7 +824,7 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
     count_launch();
     // ---- pair tiles: their number comes back, then their arrays
     if (want[2]) {
-        if (const int rc = count_pair_blocks(p, mask, cands, d_totals, chosen, heads_per_kv(p), o.pair_chunk == 0, pairs[4]); rc != LIBRA_OK)
+        if (const int rc = count_pair_blocks(p, mask, cands, d_totals, chosen, heads_per_kv(p), o.pair_chunk == 0, pairs[4], cells); rc != LIBRA_OK)
             return rc;
         Carver ps, pm;
         size_t pair_zero = 0;
@@ -837,10 +865,11 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
             max_nb = p->dir[k].NB > max_nb ? p->dir[k].NB : max_nb;
         }
     if (n > 0) {
-        if (sorted[5]) {
-            const PlanDir& d = p->dir[5];
-            k_tail_units<<<grid_for(d.NB, 256), 256, 0, s>>>(mask, p->d_blk, p->d_blk_near, d.NB - d.n_tails, d.tail_rows, d.tail_width,
-                                                             views.v[n - 1]);
+        for (int k = 5, at = n - sorted[5] - sorted[6]; k < kDirs; ++k) {
+            if (!sorted[k]) continue;
+            const PlanDir& d = p->dir[k];
+            k_tail_units<<<grid_for(d.NB, 256), 256, 0, s>>>(mask, p->d_blk, p->d_blk_near, d.NB - d.n_tails, d.tile, d.tail_rows, d.tail_width,
+                                                             views.v[at++]);
             count_launch();
         }
         k_block_weights<<<dim3(grid_for(max_nb * 32, 256), n), 256, 0, s>>>(mask, views);
@@ -850,7 +879,7 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
     const int n_sorted = n;
     // No kernel walks the lists of the 128-key pair tiles where the fused backward has its wide ones: they are made when they
     // are exported.
-    const bool listed[kDirs] = {sorted[0], sorted[1], pairs[2] && !pairs[4], sorted[3] || pairs[3], pairs[4], sorted[5]};
+    const bool listed[kDirs] = {sorted[0], sorted[1], pairs[2] && !pairs[4], sorted[3] || pairs[3], pairs[4], sorted[5], sorted[6]};
     for (int k = 2; k < kDirs; ++k)
         if (listed[k] && !sorted[k]) views.v[n++] = view_of(p->dir[k], 1, o);
     if (n == 0) return LIBRA_OK;
@@ -873,6 +902,7 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
         count_launch();
     }
     for (int k = 0; k < kDirs; ++k) p->dir[k].enabled = sorted[k] || pairs[k] ? 1 : 0;
+    if (pairs[2]) p->two_kernel = prefer_two_kernels(p, pairs[4], cells);
     return cudaGetLastError() == cudaSuccess ? LIBRA_OK : LIBRA_ERR_CUDA;
 }
 
@@ -929,16 +959,20 @@ static int make_plan(const int32_t* cu_seqlens_dev, int n_samples, int n_heads, 
     p->W = o.n_workers ? o.n_workers : sms;
     const int dirs = o.directions ? o.directions : (LIBRA_DIR_Q | LIBRA_DIR_KV);
     const int tile_kv = o.tile_kv ? o.tile_kv : 128;
+    p->asked = dirs;
+    // (windowed plans with pair tiles may take the two-kernel form)
+    const bool key_major = (dirs & LIBRA_DIR_KV) || (p->window && (dirs & LIBRA_DIR_PAIR) && (dirs & LIBRA_DIR_Q) && tile_kv == 128);
     const bool keys = (dirs & (LIBRA_DIR_KV | LIBRA_DIR_PAIR)) != 0;
-    const bool want[libra_plan::kDirs] = {(dirs & LIBRA_DIR_Q) != 0, (dirs & LIBRA_DIR_KV) != 0, (dirs & LIBRA_DIR_PAIR) != 0,
+    const bool want[libra_plan::kDirs] = {(dirs & LIBRA_DIR_Q) != 0, key_major, (dirs & LIBRA_DIR_PAIR) != 0,
                                           keys && tile_kv == 128,
                                           (dirs & LIBRA_DIR_PAIR) != 0 && tile_kv == 128 && p->W >= 2,
-                                          (dirs & LIBRA_DIR_KV) != 0 && tile_kv == 128 && p->sinks > 0};
+                                          key_major && tile_kv == 128 && p->sinks > 0,
+                                          key_major && tile_kv == 128 && p->sinks > 0 && !(dirs & LIBRA_DIR_PAIR)};
     for (int k = 0; k < libra_plan::kDirs; ++k) {
         PlanDir& d = p->dir[k];
-        d.tile = k == 0 ? tile_q : (k == 3 || k == 4 ? 256 : tile_kv);
+        d.tile = k == 0 ? tile_q : (k == 3 || k == 4 || k == 6 ? 256 : tile_kv);
         d.H = k == 0 ? n_heads : (o.n_heads_kv ? o.n_heads_kv : n_heads);
-        d.W = k == 3 ? (p->W + 1) / 2 : (k == 4 ? p->W / 2 : p->W);
+        d.W = k == 3 || k == 6 ? (p->W + 1) / 2 : (k == 4 ? p->W / 2 : p->W);
         d.chunk = k >= 2 && k <= 4 ? (o.pair_chunk ? o.pair_chunk : 4096) : 0;
         if (k == 3) {
             // The 256-wide kernels go through a tile's heads one after the other and their workers are out of step, so what
@@ -973,7 +1007,7 @@ extern "C" int libra_plan_tiles_window(const int32_t* cu_seqlens_dev, int n_samp
 }
 
 static PlanDir* dir_of(const libra_plan_t* plan, int direction) {
-    if (!plan) return nullptr;
+    if (!plan || !(plan->asked & direction)) return nullptr;
     if (direction == LIBRA_DIR_Q) return plan->dir[0].enabled ? const_cast<PlanDir*>(&plan->dir[0]) : nullptr;
     if (direction == LIBRA_DIR_KV) return plan->dir[1].enabled ? const_cast<PlanDir*>(&plan->dir[1]) : nullptr;
     if (direction == LIBRA_DIR_PAIR) return plan->dir[2].enabled ? const_cast<PlanDir*>(&plan->dir[2]) : nullptr;
@@ -1063,7 +1097,7 @@ extern "C" int libra_plan_export_pairs(const libra_plan_t* plan, int32_t* key_bl
 extern "C" int libra_plan_fused_ctas(const libra_plan_t* plan) {
     if (!plan) return LIBRA_ERR_INVALID_ARG;
     if (!plan->dir[2].enabled) return LIBRA_ERR_PLAN_MISMATCH;
-    return plan->dir[4].enabled ? 2 : 1;
+    return plan->two_kernel ? 0 : (plan->dir[4].enabled ? 2 : 1);
 }
 
 extern "C" int libra_plan_destroy(libra_plan_t* plan) {

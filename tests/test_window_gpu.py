@@ -105,6 +105,29 @@ def test_fused_backward_on_pairs_of_ctas(window, sinks):
     plan.destroy()
 
 
+def test_the_form_of_the_backward():
+    """With few key-major tiles for the workers the fused form, with many the two-kernel one, bit for bit what a plan without
+    pair tiles gives; lists that were not asked for stay the library's own."""
+    from paper_2607_23250_b200 import binding as lb
+    cu = pools.cu_seqlens([900, 300])
+    q, k, v, dout = _tensors(cu, 4, 2, 128, 2)
+    results = []
+    for workers, fused, ctas in ((148, True, 1), (12, True, 0), (12, False, None)):
+        plan = _plan(cu, 4, 2, fused, 150, 3, n_workers=workers)
+        if fused:
+            assert plan.fused_ctas() == ctas
+            with pytest.raises(lb.LibraError) as err:
+                plan.info(lb.LIBRA_DIR_KV)
+            assert err.value.code == lb.ERR_PLAN_MISMATCH
+        out, lse = lb.libra_attn_pool_fwd(q, k, v, plan)
+        ws = lb.libra_attn_pool_bwd_workspace_bytes(plan, q, k)
+        results.append((ws, lb.libra_attn_pool_bwd(q, k, v, out, lse, dout, plan)))
+        _check(cu, q, k, v, dout, (out, lse, results[-1][1]), 150, 3)
+        plan.destroy()
+    assert results[1][0] == results[2][0] < results[0][0]
+    assert all(torch.equal(x, y) for x, y in zip(results[1][1], results[2][1]))
+
+
 @pytest.mark.parametrize("d,fused", FORMS)
 def test_a_window_that_reaches_everything_changes_nothing(d, fused):
     from paper_2607_23250_b200 import binding as lb
@@ -126,7 +149,7 @@ def test_a_window_that_reaches_everything_changes_nothing(d, fused):
 
 
 @pytest.mark.parametrize("window,sinks", [(200, 1), (130, 130), (90, 300), (1, 128), (2000, 4), (128, 700)])
-@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("d", [64, 128, 256])
 def test_tails_of_sinks_in_the_two_kernel_form(d, window, sinks):
     """Key blocks with sinks whose row blocks beyond the window are tiles of their own, in one chunk and in several, of samples
     that start in the same key block as others and of one that ends inside a chunk; the same bits twice."""
@@ -138,6 +161,14 @@ def test_tails_of_sinks_in_the_two_kernel_form(d, window, sinks):
     again = _run(plan, q, k, v, dout, False)
     assert all(torch.equal(x, y) for x, y in zip(got[2], again[2]))
     plan.destroy()
+
+
+@pytest.mark.parametrize("lengths,window,sinks", [([1500], 100, 4), ([1100, 30], 300, 1), ([700], 50, 130), ([40, 900, 3], 1, 128), ([2000], 260, 2)])
+@pytest.mark.parametrize("hq,hkv", [(4, 1), (8, 1), (6, 2)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_tails_shared_by_clusters(d, hq, hkv, lengths, window, sinks):
+    """Few tiles: clusters of CTAs share the main tiles and the tails."""
+    _case(lengths, hq, hkv, d, False, window, sinks, seed=window)
 
 
 @pytest.mark.parametrize("seed", range(10))
