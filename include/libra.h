@@ -66,7 +66,8 @@ extern "C" {
 #define LIBRA_KERNEL_BWD_DQ    3   /* backward dQ kernel (walks the query-major lists)        */
 #define LIBRA_KERNEL_BWD_PREP  4   /* backward row statistics and clearing of accumulators (timing only) */
 #define LIBRA_KERNEL_BWD_FUSED 5   /* fused backward kernel (walks the pair tiles) */
-#define LIBRA_KERNEL_BWD_POST  6   /* fused backward: scaling and rounding of the accumulators (timing only)   */
+#define LIBRA_KERNEL_BWD_POST  6   /* fused backward: scaling and rounding of the accumulators; two-kernel backward with
+                                      sinks: adding up of partial sums (timing only) */
 
 typedef struct libra_plan libra_plan_t;   /* opaque, library-owned */
 
@@ -144,8 +145,8 @@ int libra_plan_tiles(const int32_t* cu_seqlens_dev, int n_samples, int n_heads, 
  * 128 walks lists of its own instead of the key-major ones, in which the row blocks beyond the window of a key block that
  * holds sinks are tiles of their own; their partial sums are added up in a fixed order, in its workspace.)
  * At head_dim 128 a plan with LIBRA_DIR_PAIR and LIBRA_DIR_Q leaves the backward's form to the library: the two-kernel form
- * (bit-reproducible, and without the fp32 accumulators in the workspace) where short windows make it the faster one,
- * libra_plan_fused_ctas then returns 0.
+ * (bit-reproducible, and without the fp32 accumulators in the workspace) where short windows make it the faster one:
+ * libra_plan_fused_ctas then returns 0, and libra_busy_times and the kernel times are those of the dK/dV and dQ kernels.
  * A window that is not below T gives what libra_plan_tiles gives, one that is not below any sample's length the same
  * results (with sinks up to rounding).  As there, an infinity or
  * a NaN of a key or value reaches rows that do not see it where they share a 128-row block with rows, and a key
@@ -299,8 +300,8 @@ typedef struct {
 /* Writes the checkpoint of the given tensors; unpack reads them back as bf16.  A tensor whose pointer (the bf16 one) is null is
  * left out, and so may its checkpoint be.  Of dims, total_tokens, hq (q, out), hkv (k, v) and head_dim count.  One launch, no
  * scratch; the tensors and the checkpoint do not overlap.  `ckpt` is a HOST struct of device pointers, read before the
- * call returns.  Errors: INVALID_ARG (also misaligned tensors or values, or a tensor without its checkpoint), UNSUPPORTED
- * (head_dim), OVERFLOW, CUDA. */
+ * call returns.  Errors: INVALID_ARG (also misaligned tensors or values, a tensor without its checkpoint, memory that is the
+ * host's or another device's than the current one), UNSUPPORTED (head_dim), OVERFLOW, CUDA. */
 int libra_ckpt8_pack(const void* q_dev, const void* k_dev, const void* v_dev, const void* out_dev,
                      const libra_ckpt8* ckpt, const libra_dims* dims, void* stream);
 int libra_ckpt8_unpack(const libra_ckpt8* ckpt, void* q_dev, void* k_dev, void* v_dev, void* out_dev,

@@ -63,23 +63,36 @@ __global__ void __launch_bounds__(kCkptThreads) k_ckpt8_unpack(const __grid_cons
     unpack_share(a.t, blockIdx.x * (kCkptThreads / 32) + (threadIdx.x >> 5));
 }
 
+// Memory that a kernel on this device may touch (there is no plan that names the device).
+static bool on_device(const void* p, int dev) {
+    cudaPointerAttributes at;
+    if (cudaPointerGetAttributes(&at, p) != cudaSuccess) { cudaGetLastError(); return false; }
+    return at.type == cudaMemoryTypeManaged || (at.type == cudaMemoryTypeDevice && at.device == dev);
+}
+
 // pack: x -> held, else held -> x.
 static int run_ckpt8(bool pack, const void* const (&x)[4], const libra_ckpt8* c, const libra_dims* dims, cudaStream_t s) {
     if (!c || !dims || dims->total_tokens <= 0 || dims->hq <= 0 || dims->hkv <= 0) return LIBRA_ERR_INVALID_ARG;
     if (dims->head_dim != 64 && dims->head_dim != 128 && dims->head_dim != 256) return LIBRA_ERR_UNSUPPORTED;
     const void* const q[4] = {c->q, c->k, c->v, c->out};
     const void* const e[4] = {c->q_exp, c->k_exp, c->v_exp, c->out_exp};
+    const int64_t rows = dims->total_tokens;
+    for (const int heads : {dims->hq, dims->hkv})
+        if ((long double)rows * heads * dims->head_dim >= 2.0e12L) return LIBRA_ERR_OVERFLOW;   // (a warp's share is numbered in 32 bits)
     CkptArgs a = {};
     int64_t warps = 0;
     for (int k = 0; k < 4; ++k) {
         const int heads = k == 0 || k == 3 ? dims->hq : dims->hkv;
-        if ((long double)dims->total_tokens * heads * dims->head_dim >= 9.0e12L) return LIBRA_ERR_OVERFLOW;
         // a tensor that is not asked for is left out, whether or not the checkpoint has it
-        if (!set_tensor(a.t[k], x[k], x[k] ? q[k] : nullptr, x[k] ? e[k] : nullptr, dims->total_tokens * heads * dims->head_dim))
+        if (!set_tensor(a.t[k], x[k], x[k] ? q[k] : nullptr, x[k] ? e[k] : nullptr, rows * heads * dims->head_dim))
             return LIBRA_ERR_INVALID_ARG;
         warps += a.t[k].chunks;
     }
     if (warps == 0) return LIBRA_OK;
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return LIBRA_ERR_NO_DEVICE; }
+    for (const CkptTensor& t : a.t)
+        if (t.chunks && !(on_device(t.x, dev) && on_device(t.q, dev) && on_device(t.e, dev))) return LIBRA_ERR_INVALID_ARG;
     const int64_t blocks = (warps + kCkptThreads / 32 - 1) / (kCkptThreads / 32);
     if (blocks > INT32_MAX / 16) return LIBRA_ERR_OVERFLOW;
     count_launch();

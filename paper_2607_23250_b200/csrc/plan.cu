@@ -960,7 +960,7 @@ static int make_plan(const int32_t* cu_seqlens_dev, int n_samples, int n_heads, 
     const int dirs = o.directions ? o.directions : (LIBRA_DIR_Q | LIBRA_DIR_KV);
     const int tile_kv = o.tile_kv ? o.tile_kv : 128;
     p->asked = dirs;
-    // (windowed plans with pair tiles may take the two-kernel form)
+    // (windowed plans with pair tiles may take the two-kernel form: prefer_two_kernels)
     const bool key_major = (dirs & LIBRA_DIR_KV) || (p->window && (dirs & LIBRA_DIR_PAIR) && (dirs & LIBRA_DIR_Q) && tile_kv == 128);
     const bool keys = (dirs & (LIBRA_DIR_KV | LIBRA_DIR_PAIR)) != 0;
     const bool want[libra_plan::kDirs] = {(dirs & LIBRA_DIR_Q) != 0, key_major, (dirs & LIBRA_DIR_PAIR) != 0,
@@ -1006,12 +1006,17 @@ extern "C" int libra_plan_tiles_window(const int32_t* cu_seqlens_dev, int n_samp
     return make_plan(cu_seqlens_dev, n_samples, n_heads, tile_q, opts, window, sinks, stream, plan_out);
 }
 
-static PlanDir* dir_of(const libra_plan_t* plan, int direction) {
-    if (!plan || !(plan->asked & direction)) return nullptr;
+static PlanDir* any_dir(const libra_plan_t* plan, int direction) {
+    if (!plan) return nullptr;
     if (direction == LIBRA_DIR_Q) return plan->dir[0].enabled ? const_cast<PlanDir*>(&plan->dir[0]) : nullptr;
     if (direction == LIBRA_DIR_KV) return plan->dir[1].enabled ? const_cast<PlanDir*>(&plan->dir[1]) : nullptr;
     if (direction == LIBRA_DIR_PAIR) return plan->dir[2].enabled ? const_cast<PlanDir*>(&plan->dir[2]) : nullptr;
     return nullptr;
+}
+
+// A direction that the caller asked for.
+static PlanDir* dir_of(const libra_plan_t* plan, int direction) {
+    return plan && (plan->asked & direction) ? any_dir(plan, direction) : nullptr;
 }
 
 extern "C" int libra_plan_info(const libra_plan_t* plan, int direction, int64_t* n_tiles, int* n_workers,
@@ -1126,8 +1131,8 @@ extern "C" int libra_busy_times(const libra_plan_t* plan, int which, uint64_t* n
     if ((which < LIBRA_KERNEL_FWD || which > LIBRA_KERNEL_BWD_DQ) && which != LIBRA_KERNEL_BWD_FUSED) return LIBRA_ERR_INVALID_ARG;
     // the forward and the dQ kernel walk the query-major lists, the dK/dV kernel the key-major ones, the fused
     // backward the pair tiles
-    PlanDir* d = dir_of(plan, which == LIBRA_KERNEL_BWD_FUSED ? LIBRA_DIR_PAIR
-                                                              : (which == LIBRA_KERNEL_BWD_DKDV ? LIBRA_DIR_KV : LIBRA_DIR_Q));
+    PlanDir* d = any_dir(plan, which == LIBRA_KERNEL_BWD_FUSED ? LIBRA_DIR_PAIR
+                                                               : (which == LIBRA_KERNEL_BWD_DKDV ? LIBRA_DIR_KV : LIBRA_DIR_Q));
     if (!d) return LIBRA_ERR_PLAN_MISMATCH;
     if (cudaDeviceSynchronize() != cudaSuccess) return LIBRA_ERR_CUDA;
     const size_t most = (size_t)d->W + 1;
@@ -1156,7 +1161,7 @@ extern "C" int libra_busy_times(const libra_plan_t* plan, int which, uint64_t* n
 extern "C" int libra_tile_times(const libra_plan_t* plan, int which, uint32_t* ns_host) {
     if (!plan || !ns_host) return LIBRA_ERR_INVALID_ARG;
     if (which != LIBRA_KERNEL_FWD && which != LIBRA_KERNEL_BWD_FUSED) return LIBRA_ERR_INVALID_ARG;
-    PlanDir* d = dir_of(plan, which == LIBRA_KERNEL_BWD_FUSED ? LIBRA_DIR_PAIR : LIBRA_DIR_Q);
+    PlanDir* d = any_dir(plan, which == LIBRA_KERNEL_BWD_FUSED ? LIBRA_DIR_PAIR : LIBRA_DIR_Q);
     if (!d) return LIBRA_ERR_PLAN_MISMATCH;
     if (cudaDeviceSynchronize() != cudaSuccess) return LIBRA_ERR_CUDA;
     return cudaMemcpy(ns_host, d->d_tile_ns, sizeof(uint32_t) * d->NT, cudaMemcpyDeviceToHost) == cudaSuccess

@@ -58,7 +58,7 @@ def test_bad_arguments_are_refused_before_any_cuda_call():
             assert call(full, ctypes.byref(bad), x) == -1
         for d in (0, 32, 96, 192, 512):
             assert call(full, ctypes.byref(Dims(10, 1, 2, 1, d, 0)), x) == -2
-        assert call(full, ctypes.byref(Dims(1 << 40, 1, 1 << 10, 1, 64, 0)), x) == -5
+        assert call(full, ctypes.byref(Dims(1 << 30, 1, 1 << 10, 1, 64, 0)), x) == -5
         assert call(full, ctypes.byref(dims), args) == 0                       # nothing asked for
         for k in range(8):                                                     # a tensor without its values or exponents
             part = Held(*[0 if i == k else 256 for i in range(8)])

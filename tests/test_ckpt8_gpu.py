@@ -75,6 +75,20 @@ def test_parts_of_a_layer_and_tensors_given():
     assert err.value.code == lb.ERR_UNSUPPORTED
 
 
+def test_host_memory_is_refused():
+    from paper_2607_23250_b200 import binding as lb
+    import ctypes
+    x = torch.zeros((8, 1, 64), dtype=torch.bfloat16)
+    held, exps = torch.zeros((8, 1, 64), dtype=torch.int8, device="cuda"), torch.zeros((8, 1, 2), dtype=torch.uint8, device="cuda")
+    c = lb._Ckpt8Pointers(held.data_ptr(), None, None, None, exps.data_ptr(), None, None, None)
+    dims = lb.Dims(8, 0, 1, 1, 64, 0.0)
+    null = ctypes.c_void_p(0)
+    for call in (lambda p: lb._lib.libra_ckpt8_pack(p, null, null, null, ctypes.byref(c), ctypes.byref(dims), None),
+                 lambda p: lb._lib.libra_ckpt8_unpack(ctypes.byref(c), p, null, null, null, ctypes.byref(dims), None)):
+        for mem in (x, x.pin_memory()):
+            assert call(ctypes.c_void_p(mem.data_ptr())) == lb.ERR_INVALID_ARG
+
+
 LENGTHS = [150, 1, 700, 33, 260]
 
 

@@ -68,7 +68,7 @@ def test_sample_bounds_at_word_and_block_edges(d, fused, window, sinks):
 @pytest.mark.parametrize("lengths,window,sinks", [
     ([1], 1, 0), ([1], 5, 5), ([2, 1], 1, 1), ([257], 3, 300), ([1500], 100, 4), ([1500], 500, 0), ([1500], 300, 260),
     ([700, 40, 900], 129, 129), ([100, 1400], 384, 130), ([1000, 600], 640, 1), ([1600], 1599, 0), ([1600], 1, 1599),
-    ([130, 1, 1, 1400, 3], 257, 7)])
+    ([130, 1, 1, 1400, 3], 257, 7), ([300, 0, 0, 500, 0, 120], 90, 3)])
 @pytest.mark.parametrize("d,fused", FORMS)
 def test_long_and_mixed_samples(d, fused, lengths, window, sinks):
     _case(lengths, 4, 2, d, fused, window, sinks, seed=sum(lengths))
@@ -287,4 +287,39 @@ def test_stalled_producers_give_up_cleanly(d):
     plan.set_wait_limit_ns(0)
     again = _run(plan, q, k, v, dout, False)
     assert torch.equal(good[0], again[0]) and all(torch.equal(x, y) for x, y in zip(good[2], again[2]))
+    plan.destroy()
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+@pytest.mark.parametrize("d,fused", FORMS)
+def test_values_that_are_not_finite_stay_near(d, fused, value):
+    """Products are taken a block of 128 keys by a tile of 256 rows at a time, masked ones with a weight of 0: a key and a value that are
+    not finite reach the tiles of rows that see a key of their block (the block's last key by a window's length), a query
+    and its gradient the 256-key tiles of keys that a row of its block sees, the sinks' among them.  Everything else is what it was."""
+    T, window, sinks, at = 2300, 300, 4, 900
+    cu = pools.cu_seqlens([T])
+    q, k, v, dout = _tensors(cu, 2, 1, d, 6)
+    plan = _plan(cu, 2, 1, fused, window, sinks)
+    out, lse, grads = _run(plan, q, k, v, dout, fused)
+    tile = lambda t: t // 256 * 256  # noqa: E731
+    block = at // 128 * 128
+    near = slice(tile(at), tile(block + 127 + window - 1) + 256)
+    k2, v2 = k.clone(), v.clone()
+    k2[at], v2[at, 0, 5] = value, value
+    out2, lse2, _ = _run(plan, q, k2, v2, dout, fused)
+    far = torch.ones(T, dtype=torch.bool, device="cuda")
+    far[near] = False
+    assert torch.equal(out[far], out2[far]) and torch.equal(lse[:, far], lse2[:, far])
+    from paper_2607_23250_b200 import binding as lb
+    g2 = dout.clone()
+    g2[at] = value
+    dq, dk, dv = lb.libra_attn_pool_bwd(q, k, v, out, lse, g2, plan)
+    far = torch.ones(T, dtype=torch.bool, device="cuda")
+    far[tile(at)] = False
+    far[tile(at):tile(at) + 256] = False
+    same = torch.equal if not fused else lambda x, y: bool((x - y).abs().max() <= 2.0 ** -6 * y.abs().max())
+    assert same(dq[far], grads[0][far])
+    far[tile(block - window + 1):tile(at) + 256] = False
+    far[:256] = False                                                   # the sinks' tile
+    assert same(dk[far], grads[1][far]) and same(dv[far], grads[2][far])
     plan.destroy()
