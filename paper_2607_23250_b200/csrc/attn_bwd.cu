@@ -711,7 +711,7 @@ __global__ void k_bwd_prep(const void* __restrict__ out_, const uint8_t* __restr
     const uint32_t rare = blockIdx.x < mix.spread ? turn : mix.spread / mix.period, usual = blockIdx.x - rare - (blockIdx.x < mix.spread);
     if (odd == mix.clear_is_rare) {
         if (HELD && (odd ? rare : usual) >= restore.n_clear_ctas) {
-            unpack_share(restore.t, ((odd ? rare : usual) - restore.n_clear_ctas) * 8 + (threadIdx.x >> 5));
+            unpack_shares<kRestoreShares>(restore.t, ((odd ? rare : usual) - restore.n_clear_ctas) * 8 + (threadIdx.x >> 5));
             return;
         }
         int64_t i = (int64_t)(odd ? rare : usual) * (256 * kClearPerThread) + threadIdx.x;
@@ -732,49 +732,78 @@ __global__ void k_bwd_prep(const void* __restrict__ out_, const uint8_t* __restr
     for (int round = 0; round < rounds; ++round) {
         const int64_t t0 = ((int64_t)(w % groups) * rounds + round) * ROWS;
         float mine = 0.f;
-        uint4 a[STEPS], b[STEPS];   // (HELD: two words of a are used)
-        uint32_t e[HELD ? STEPS : 1];
+        if constexpr (HELD) {
+            // Sixteen values a lane, so that as many bytes are under way as with bf16: eight (and 120 registers for all steps of them, or
+            // two batches) read 1.63 GB in 409 us, 363 so.  The two halves' sums are added last: bit for bit the sum below.
+            constexpr int LPRH = D / 16, RPSH = 32 / LPRH, STEPSH = ROWS / RPSH;
+            const int subh = lane / LPRH, parth = lane % LPRH;
+            uint4 a[STEPSH], b[STEPSH][2];
+            uint32_t e[STEPSH];
 #pragma unroll
-        for (int u = 0; u < STEPS; ++u) {
-            const int64_t t = t0 + u * RPS + sub;
-            a[u] = b[u] = make_uint4(0, 0, 0, 0);
-            if (HELD) e[u % (HELD ? STEPS : 1)] = 7;
-            if (t < T) {
-                if constexpr (HELD) {
+            for (int u = 0; u < STEPSH; ++u) {
+                const int64_t t = t0 + u * RPSH + subh;
+                a[u] = b[u][0] = b[u][1] = make_uint4(0, 0, 0, 0);
+                e[u] = 7;
+                if (t < T) {
                     const size_t row = (size_t)t * hq + h;
-                    const uint2 x = __ldg(reinterpret_cast<const uint2*>(static_cast<const int8_t*>(out_) + row * D) + part);
-                    a[u].x = x.x;
-                    a[u].y = x.y;
-                    e[u] = __ldg(out_exp + row * (D / kRun) + part / (kRun / 8));
-                } else {
-                    a[u] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(out_) + ((size_t)t * hq + h) * D) + part);
+                    a[u] = __ldg(reinterpret_cast<const uint4*>(static_cast<const int8_t*>(out_) + row * D) + parth);
+                    const uint4* y = reinterpret_cast<const uint4*>(dout + row * D) + 2 * parth;
+                    b[u][0] = __ldg(y);
+                    b[u][1] = __ldg(y + 1);
+                    e[u] = __ldg(out_exp + row * (D / kRun) + parth / (kRun / 16));
                 }
-                b[u] = __ldg(reinterpret_cast<const uint4*>(dout + ((size_t)t * hq + h) * D) + part);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < STEPS; ++u) {
-            const uint32_t* x = reinterpret_cast<const uint32_t*>(&a[u]);
-            const uint32_t* y = reinterpret_cast<const uint32_t*>(&b[u]);
-            float acc = 0.f;
-            float held[8];
-            if constexpr (HELD) {
-                held_floats(x[0], held);
-                held_floats(x[1], held + 4);
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 fa = HELD ? make_float2(held[2 * i], held[2 * i + 1])
-                                       : __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x[i]));
-                const float2 fb = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&y[i]));
-                acc += fa.x * fb.x + fa.y * fb.y;
-            }
-            if constexpr (HELD) acc *= run_up(e[u]);
+            for (int u = 0; u < STEPSH; ++u) {
+                const uint32_t* x = reinterpret_cast<const uint32_t*>(&a[u]);
+                float acc[2];
 #pragma unroll
-            for (int off = LPR / 2; off > 0; off >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, off);
-            // row u * RPS + sub of the warp's goes to the lane of that number
-            const float got = __shfl_sync(0xffffffffu, acc, (lane % RPS) * LPR);
-            if (lane / RPS == u) mine = got;
+                for (int k = 0; k < 2; ++k) {
+                    const uint32_t* y = reinterpret_cast<const uint32_t*>(&b[u][k]);
+                    float held[8];
+                    held_floats(x[2 * k], held);
+                    held_floats(x[2 * k + 1], held + 4);
+                    acc[k] = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 fb = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&y[i]));
+                        acc[k] += held[2 * i] * fb.x + held[2 * i + 1] * fb.y;
+                    }
+                    acc[k] *= run_up(e[u]);
+#pragma unroll
+                    for (int off = LPRH / 2; off > 0; off >>= 1) acc[k] += __shfl_xor_sync(0xffffffffu, acc[k], off);
+                }
+                const float got = __shfl_sync(0xffffffffu, acc[0] + acc[1], (lane % RPSH) * LPRH);
+                if (lane / RPSH == u) mine = got;
+            }
+        } else {
+            uint4 a[STEPS], b[STEPS];
+#pragma unroll
+            for (int u = 0; u < STEPS; ++u) {
+                const int64_t t = t0 + u * RPS + sub;
+                a[u] = b[u] = make_uint4(0, 0, 0, 0);
+                if (t < T) {
+                    a[u] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(out_) + ((size_t)t * hq + h) * D) + part);
+                    b[u] = __ldg(reinterpret_cast<const uint4*>(dout + ((size_t)t * hq + h) * D) + part);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < STEPS; ++u) {
+                const uint32_t* x = reinterpret_cast<const uint32_t*>(&a[u]);
+                const uint32_t* y = reinterpret_cast<const uint32_t*>(&b[u]);
+                float acc = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 fa = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x[i]));
+                    const float2 fb = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&y[i]));
+                    acc += fa.x * fb.x + fa.y * fb.y;
+                }
+#pragma unroll
+                for (int off = LPR / 2; off > 0; off >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, off);
+                // row u * RPS + sub of the warp's goes to the lane of that number
+                const float got = __shfl_sync(0xffffffffu, acc, (lane % RPS) * LPR);
+                if (lane / RPS == u) mine = got;
+            }
         }
         if (lane < ROWS) {
             const int64_t t = t0 + lane;
@@ -942,7 +971,7 @@ static cudaError_t launch_prep(const RowsOut& out, const void* dout, const float
     RestoreArgs restore = out.restore;
     if (out.held) {
         restore.n_clear_ctas = (uint32_t)clearers;
-        clearers += (restore.t[0].chunks + restore.t[1].chunks + restore.t[2].chunks + 7) / 8;
+        clearers += (restore.t[0].chunks + restore.t[1].chunks + restore.t[2].chunks + 8 * kRestoreShares - 1) / (8 * kRestoreShares);
     }
     const int64_t rare = clearers < readers ? clearers : readers, usual = clearers + readers - rare;
     PrepMix mix;

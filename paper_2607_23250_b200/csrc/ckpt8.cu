@@ -2,8 +2,8 @@
 // pass (format: ckpt8.cuh).
 //
 // Both directions are bound by memory: 2 bytes a value on one side, 33 / 32 on the other.  A warp takes kWarpRuns runs of 32
-// values: four lanes a run, 16 bytes of bf16 and 8 of integers a lane, all loads issued before the first is used, and
-// the runs' exponent bytes as one 32-byte access.  The tensors of a call share a launch.
+// values, issues all of its loads before the first is used and takes the runs' exponent bytes as one 32-byte access.  The tensors
+// of a call share a launch.  There and back, 131072 tokens, 32 / 8 heads of 128: 598 + 596 us, 6.8 TB/s.
 #include "common.h"
 #include "ckpt8.cuh"
 
@@ -15,52 +15,66 @@ struct CkptArgs {
     CkptTensor t[4];
 };
 
+// Eight values as integers: 1.5 2^23 + y has rint(y) in its low bits, ties to even.
+__device__ __forceinline__ uint2 quant8(const uint4& x, float down) {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(&x);
+    uint32_t q[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint32_t b[4];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float lo = __uint_as_float(w[2 * i + j] << 16) * down, hi = __uint_as_float(w[2 * i + j] & 0xffff0000u) * down;
+            b[2 * j] = __float_as_uint(fminf(fmaxf(lo, -127.f), 127.f) + 12582912.0f);
+            b[2 * j + 1] = __float_as_uint(fminf(fmaxf(hi, -127.f), 127.f) + 12582912.0f);
+        }
+        q[i] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+    }
+    return make_uint2(q[0], q[1]);
+}
+// Two lanes a run: 16 bytes of integers a lane.  (Four lanes a run, as in unpack_shares, with streaming loads and stores: 660 us for
+// 131072 tokens, 32 / 8 heads of 128; so with them 631, without 598, 6.8 TB/s; blocks of 1024 threads 830.)
 __global__ void __launch_bounds__(kCkptThreads) k_ckpt8_pack(const __grid_constant__ CkptArgs a) {
     grid_dep_wait();
     int64_t run0;
     const CkptTensor t = share_of(a.t, blockIdx.x * (kCkptThreads / 32) + (threadIdx.x >> 5), run0);
     if (run0 >= t.runs) return;
     const int lane = threadIdx.x & 31;
-    const int64_t at = run0 * 4 + lane;         // this lane's eight values of step 0
-    uint4 x[kSteps];
+    uint4 x[2][2];                              // two lanes a run, 16 values of it each, two steps
 #pragma unroll
-    for (int u = 0; u < kSteps; ++u) {
-        x[u] = make_uint4(0, 0, 0, 0);
-        if (run0 + 8 * u + (lane >> 2) < t.runs) x[u] = __ldcs(t.x + at + 32 * u);
+    for (int u = 0; u < 2; ++u) {
+        x[u][0] = x[u][1] = make_uint4(0, 0, 0, 0);
+        if (run0 + 16 * u + (lane >> 1) < t.runs) {
+            const uint4* src = t.x + (run0 + 16 * u) * 4 + 2 * lane;
+            x[u][0] = __ldg(src);
+            x[u][1] = __ldg(src + 1);
+        }
     }
     uint32_t mine = 0;                          // exponent of run `lane`
 #pragma unroll
-    for (int u = 0; u < kSteps; ++u) {
-        const uint32_t* w = reinterpret_cast<const uint32_t*>(&x[u]);
-        uint32_t m = __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+    for (int u = 0; u < 2; ++u) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint32_t* w = reinterpret_cast<const uint32_t*>(&x[u][k]);
+            m = __vmaxu2(m, __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu)));
+        }
         m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 1));
-        m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 2));
         uint32_t e = max(m & 0xffffu, m >> 16) >> 7;
         e = e < 7 ? 7 : e;
         const float down = run_down(e);
-        uint32_t q[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            uint32_t b[4];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                // 1.5 2^23 + y has rint(y) in its low bits, ties to even
-                const float lo = __uint_as_float(w[2 * i + j] << 16) * down, hi = __uint_as_float(w[2 * i + j] & 0xffff0000u) * down;
-                b[2 * j] = __float_as_uint(fminf(fmaxf(lo, -127.f), 127.f) + 12582912.0f);
-                b[2 * j + 1] = __float_as_uint(fminf(fmaxf(hi, -127.f), 127.f) + 12582912.0f);
-            }
-            q[i] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
-        }
-        const uint32_t got = __shfl_sync(0xffffffffu, e, (lane & 7) * 4);
-        if ((lane >> 3) == u) mine = got;
-        if (run0 + 8 * u + (lane >> 2) < t.runs) __stcs(t.q + at + 32 * u, make_uint2(q[0], q[1]));
+        const uint2 q0 = quant8(x[u][0], down), q1 = quant8(x[u][1], down);
+        const uint32_t got = __shfl_sync(0xffffffffu, e, (lane & 15) * 2);
+        if ((lane >> 4) == u) mine = got;
+        if (run0 + 16 * u + (lane >> 1) < t.runs) 
+            reinterpret_cast<uint4*>(t.q)[(run0 + 16 * u) * 2 + lane] = make_uint4(q0.x, q0.y, q1.x, q1.y);
     }
     if (run0 + lane < t.runs) t.e[run0 + lane] = (uint8_t)mine;
 }
 
 __global__ void __launch_bounds__(kCkptThreads) k_ckpt8_unpack(const __grid_constant__ CkptArgs a) {
     grid_dep_wait();
-    unpack_share(a.t, blockIdx.x * (kCkptThreads / 32) + (threadIdx.x >> 5));
+    unpack_shares<1>(a.t, blockIdx.x * (kCkptThreads / 32) + (threadIdx.x >> 5));
 }
 
 // Memory that a kernel on this device may touch (there is no plan that names the device).

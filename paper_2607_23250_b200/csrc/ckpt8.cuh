@@ -32,10 +32,13 @@ __device__ __forceinline__ void held_floats(uint32_t w, float* f) {
     for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7540 + i)) - 8388736.0f;
 }
 
-// How warps share a call's tensors: kWarpRuns runs of one of them each, four lanes a run, 16 bytes of bf16 and 8 of integers a
+// How warps share a call's tensors: kWarpRuns runs of one of them each; read back four lanes a run, 16 bytes of bf16 and 8 of integers a
 // lane and step; the runs' exponents are one 32-byte access.
 constexpr int kSteps = 4;                       // runs a lane takes part in
 constexpr int kWarpRuns = 8 * kSteps;
+// Of a warp of the kernel that restores q, k and v among the row statistics: its CTAs have the registers of that kernel, so fewer
+// warps fit an SM.  Both together, 65536 tokens, 8 / 2 heads of 128: 111 us with one share a warp, 103 with two, 90 with four (0.51 GB).
+constexpr int kRestoreShares = 4;
 
 struct CkptTensor {
     uint4* x;               // bf16, 8 values each
@@ -57,24 +60,27 @@ __device__ __forceinline__ CkptTensor share_of(const CkptTensor (&all)[N], uint3
     run0 = (int64_t)w * kWarpRuns;
     return t;
 }
-// Reads warp w's share back as bf16.
-template <int N>
-__device__ __forceinline__ void unpack_share(const CkptTensor (&all)[N], uint32_t w_) {
+// Reads the shares M w .. M w + M - 1 back as bf16 (all of one tensor: its shares are counted in multiples of M), the loads of all of
+// them first.
+template <int M, int N>
+__device__ __forceinline__ void unpack_shares(const CkptTensor (&all)[N], uint32_t w_) {
     int64_t run0;
-    const CkptTensor t = share_of(all, w_, run0);
+    const CkptTensor t = share_of(all, M * w_, run0);
     if (run0 >= t.runs) return;
     const int lane = threadIdx.x & 31;
     const int64_t at = run0 * 4 + lane;
-    uint2 q[kSteps];
+    uint2 q[M * kSteps];
+    uint32_t mine[M];
 #pragma unroll
-    for (int u = 0; u < kSteps; ++u) {
+    for (int u = 0; u < M * kSteps; ++u) {
         q[u] = make_uint2(0, 0);
         if (run0 + 8 * u + (lane >> 2) < t.runs) q[u] = __ldcs(t.q + at + 32 * u);
     }
-    const uint32_t mine = run0 + lane < t.runs ? t.e[run0 + lane] : 7u;
 #pragma unroll
-    for (int u = 0; u < kSteps; ++u) {
-        const float up = run_up(__shfl_sync(0xffffffffu, mine, 8 * u + (lane >> 2)));
+    for (int k = 0; k < M; ++k) mine[k] = run0 + 32 * k + lane < t.runs ? t.e[run0 + 32 * k + lane] : 7u;
+#pragma unroll
+    for (int u = 0; u < M * kSteps; ++u) {
+        const float up = run_up(__shfl_sync(0xffffffffu, mine[u / kSteps], 8 * (u % kSteps) + (lane >> 2)));
         float f[8];
         held_floats(q[u].x, f);
         held_floats(q[u].y, f + 4);
@@ -86,7 +92,7 @@ __device__ __forceinline__ void unpack_share(const CkptTensor (&all)[N], uint32_
 }
 
 // One tensor of a call: null everywhere = left out.  Returns false where only some of its pointers are given or misaligned.
-inline bool set_tensor(CkptTensor& t, const void* x, const void* q, const void* e, int64_t values) {
+inline bool set_tensor(CkptTensor& t, const void* x, const void* q, const void* e, int64_t values, int shares = 1) {
     t = {};
     if (!x && !q && !e) return true;
     if (!x || !q || !e || (((uintptr_t)x | (uintptr_t)q) & 15)) return false;
@@ -94,15 +100,16 @@ inline bool set_tensor(CkptTensor& t, const void* x, const void* q, const void* 
     t.q = (uint2*)q;
     t.e = (uint8_t*)e;
     t.runs = values / kRun;
-    t.chunks = (uint32_t)((t.runs + kWarpRuns - 1) / kWarpRuns);
+    t.chunks = (uint32_t)((t.runs + shares * kWarpRuns - 1) / (shares * kWarpRuns) * shares);   // (the last ones may be empty)
     return true;
 }
 
 // q, k and v of a checkpoint and where they are restored.
 inline bool set_restore(CkptTensor (&t)[3], const libra_ckpt8* c, void* q, void* k, void* v, const libra_dims* dims) {
     const int64_t row = dims->total_tokens * dims->head_dim;
-    return set_tensor(t[0], q, c->q, c->q_exp, row * dims->hq) && set_tensor(t[1], k, c->k, c->k_exp, row * dims->hkv) &&
-           set_tensor(t[2], v, c->v, c->v_exp, row * dims->hkv);
+    return set_tensor(t[0], q, c->q, c->q_exp, row * dims->hq, kRestoreShares) &&
+           set_tensor(t[1], k, c->k, c->k_exp, row * dims->hkv, kRestoreShares) &&
+           set_tensor(t[2], v, c->v, c->v_exp, row * dims->hkv, kRestoreShares);
 }
 
 }  // namespace libra
