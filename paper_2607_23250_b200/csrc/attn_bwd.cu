@@ -1033,15 +1033,20 @@ static int launch_fused(const void* q_dev, const void* k_dev, const void* v_dev,
         if (rc == LIBRA_OK) rc = make_thd_map(&tdo64, dout_dev, T, dims->hq, 128, 64);
         if (rc != LIBRA_OK) return rc;
         if (!cfg_done(7)) {
-            if (set_smem(k_attn_bwd_pair, PairSmem::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
-            cudaFuncAttributes a;   // the register pool: what the dQ group and the last warps release must cover the rest
-            if (cudaFuncGetAttributes(&a, k_attn_bwd_pair) != cudaSuccess) return LIBRA_ERR_CUDA;
-            const long long wanted = 2LL * (kPrRegsExp - a.numRegs) + (kPrRegsDs - a.numRegs);
-            if (a.numRegs < kPrRegsDq || a.numRegs < kPrRegsOther || wanted > 2LL * a.numRegs - kPrRegsDq - kPrRegsOther)
-                return LIBRA_ERR_UNSUPPORTED;
+            auto configure = [](auto kernel) -> int {
+                if (set_smem(kernel, PairSmem::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
+                cudaFuncAttributes a;   // the register pool: what the dQ group and the last warps release must cover the rest
+                if (cudaFuncGetAttributes(&a, kernel) != cudaSuccess) return LIBRA_ERR_CUDA;
+                const long long wanted = 2LL * (kPrRegsExp - a.numRegs) + (kPrRegsDs - a.numRegs);
+                return a.numRegs < kPrRegsDq || a.numRegs < kPrRegsOther || wanted > 2LL * a.numRegs - kPrRegsDq - kPrRegsOther
+                           ? LIBRA_ERR_UNSUPPORTED : LIBRA_OK;
+            };
+            rc = configure(k_attn_bwd_pair<false>);
+            if (rc == LIBRA_OK) rc = configure(k_attn_bwd_pair<true>);
+            if (rc != LIBRA_OK) return rc;
             cfg_mark(7);
         }
-        PairParams pp;
+        PairSinkParams pp;
         pp.lse2 = lse2; pp.dvec = dvec;
         pp.cta_offsets = wide.d_cta_offsets; pp.cta_tiles = wide.d_cta_exec;
         pp.u_blk = wide.d_u_blk; pp.u_chunk = wide.d_u_chunk; pp.tok_end = plan->d_tok_end;
@@ -1056,8 +1061,10 @@ static int launch_fused(const void* q_dev, const void* k_dev, const void* v_dev,
         pp.sink_j = d.d_sink_j; pp.sink_n = d.d_sink_n;
         mp->n_outcome[1] = 2 * wide.W;
         time_begin(mp, 4, s);
-        e = launch_dependent(k_attn_bwd_pair, 2 * wide.W, kPairThreads, PairSmem::kBytes, s, tq, tk, tv, tdo, tq64, tdo64, tacc, tdkacc,
-                             tdvacc, pp);
+        auto launch = [&](auto kernel) {
+            return launch_dependent(kernel, 2 * wide.W, kPairThreads, PairSmem::kBytes, s, tq, tk, tv, tdo, tq64, tdo64, tacc, tdkacc, tdvacc, pp);
+        };
+        e = plan->sinks ? launch(k_attn_bwd_pair<true>) : launch(k_attn_bwd_pair<false>);
     } else {
         if (!cfg_done(4)) {
             if (set_smem(k_attn_bwd_fused, FusedSmem::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;

@@ -100,46 +100,70 @@ struct PairParams {
     uint32_t wait_limit_ns;
     int inject_stall;         // test aid: the odd CTAs' producers issue no loads
     uint64_t* busy;
-    // times by 128-key pair tiles, the halves of the wide ones (same chunks): tile h NU128 + base[c] + j - first_j[c]; with
-    // sinks the sink_n[c] blocks from sink_j[c] come first (null without)
+    // times by 128-key pair tiles, the halves of the wide ones (same chunks): tile h NU128 + base[c] + j - first_j[c]
     uint32_t* tile_ns;
     const int32_t* first_j;
     const int64_t* base;
-    const int32_t* sink_j;
-    const int32_t* sink_n;
     int64_t NU128;
     // tile of a head for key block j of chunk c
+    __device__ __forceinline__ int64_t tile128(int c, int j) const { return base[c] + j - first_j[c]; }
+};
+// Of plans with sinks: the sink_n[c] blocks from sink_j[c] on come first of a chunk's.
+struct PairSinkParams : PairParams {
+    const int32_t* sink_j;
+    const int32_t* sink_n;
     __device__ __forceinline__ int64_t tile128(int c, int j) const {
-        const int n = sink_n ? sink_n[c] : 0;
-        return base[c] + (j < first_j[c] ? j - (n ? sink_j[c] : 0) : n + j - first_j[c]);
+        const int n = sink_n[c];
+        return base[c] + (j < first_j[c] ? j - sink_j[c] : n + j - first_j[c]);
     }
 };
 
 // The row blocks [i0, i0 + n_blk) that a wide pair tile walks for every head of its group.
-struct PairUnit {
+template <bool SINK>
+struct PairUnitLast {};
+template <>
+struct PairUnitLast<true> { int last1; };   // last row block that sees the upper key block: with sinks not always the unit's
+template <bool SINK>
+struct PairUnit : PairUnitLast<SINK> {
     int kvh, c, j0, i0, n_blk;
-    int last0, last1;         // last row blocks that see the lower and the upper key block (sinks: in either order)
+    int last0;                // last row block that sees the lower key block
     bool two;                 // the upper key block exists
     // row blocks of it that see key block j0 + r
     __device__ __forceinline__ int seen(uint32_t r) const {
-        const int end = i0 + n_blk;
+        int end = i0 + n_blk;
         if (r == 0) return (last0 < end ? last0 + 1 : end) - i0;
-        return two ? (last1 < end ? last1 + 1 : end) - (i0 > j0 ? i0 : j0 + 1) : 0;
+        if constexpr (SINK) end = this->last1 < end ? this->last1 + 1 : end;
+        return two ? end - (i0 > j0 ? i0 : j0 + 1) : 0;
     }
     // bit r: row block i sees key block j0 + r
-    __device__ __forceinline__ uint32_t see(int i) const { return (i <= last0 ? 1u : 0u) | (two && i > j0 && i <= last1 ? 2u : 0u); }
+    __device__ __forceinline__ uint32_t see(int i) const {
+        bool upper = two && i > j0;
+        if constexpr (SINK) upper = upper && i <= this->last1;
+        return (i <= last0 ? 1u : 0u) | (upper ? 2u : 0u);
+    }
 };
-__device__ __forceinline__ PairUnit pair_unit(const PairParams& p, int t) {
-    PairUnit u;
+template <bool SINK>
+__device__ __forceinline__ PairUnit<SINK> pair_unit(const PairParams& p, int t) {
+    PairUnit<SINK> u;
     u.kvh = t / p.NU;
     const int pb = t - u.kvh * p.NU;
     u.j0 = 2 * p.u_blk[pb];
     u.c = p.u_chunk[pb];
     const int64_t k1 = (int64_t)(u.j0 + 1) * kBlk;
-    u.last0 = last_q_block(p.blk, (int64_t)u.j0 * kBlk);
+    // (Without sinks the last key's tok_end is the largest of its block and the first key's the smallest.  Those read here instead of
+    // p.blk: two samples of 65536 tokens, 32 / 8 heads: this kernel 164.9 -> 160.0 ms; the code around them comes out differently.)
+    auto last_block = [&](int64_t k0) {
+        if constexpr (SINK) return last_q_block(p.blk, k0);
+        const int64_t last_key = (k0 + kBlk <= p.T ? k0 + kBlk : p.T) - 1;
+        return (p.tok_end[last_key] - 1) / kBlk;
+    };
+    u.last0 = last_block((int64_t)u.j0 * kBlk);
     u.two = k1 < p.T;
-    u.last1 = u.two ? last_q_block(p.blk, k1) : u.last0;
-    const int last = u.last1 > u.last0 ? u.last1 : u.last0;
+    int last = u.two ? last_block(k1) : u.last0;
+    if constexpr (SINK) {
+        u.last1 = last;
+        last = last > u.last0 ? last : u.last0;
+    }
     const int lo = u.c * p.R > u.j0 ? u.c * p.R : u.j0;
     const int hi = u.c * p.R + p.R - 1 < last ? u.c * p.R + p.R - 1 : last;
     u.i0 = lo;
@@ -164,12 +188,13 @@ __device__ __forceinline__ void warp_arrive_cluster(uint32_t bar, int lane) {
     __syncwarp();
     if (lane == 0) mbar_arrive_cluster(bar);
 }
+template <bool SINK>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 k_attn_bwd_pair(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                 const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_do,
                 const __grid_constant__ CUtensorMap tm_q64, const __grid_constant__ CUtensorMap tm_do64,
                 const __grid_constant__ CUtensorMap tm_dqacc, const __grid_constant__ CUtensorMap tm_dkacc,
-                const __grid_constant__ CUtensorMap tm_dvacc, const PairParams p) {
+                const __grid_constant__ CUtensorMap tm_dvacc, const std::conditional_t<SINK, PairSinkParams, PairParams> p) {
     using L = PairSmem;
     extern __shared__ __align__(1024) uint8_t smem[];
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBarOff);
@@ -254,7 +279,7 @@ k_attn_bwd_pair(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             uint32_t n = 0, armed = 0;
             bool ok = true;
             for (int idx = unit_begin; idx < unit_end && ok; ++idx) {
-                const PairUnit u = pair_unit(p, p.cta_tiles[idx]);
+                const PairUnit<SINK> u = pair_unit<SINK>(p, p.cta_tiles[idx]);
                 const int n_it = G * u.n_blk;
                 for (int it = 0; it < n_it; ++it) {
                     mbar_arrive_expect_tx(&bars[L::kDsIn], L::kHalf);
@@ -282,7 +307,7 @@ k_attn_bwd_pair(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             int idx = p.inject_stall && rank == 1 ? unit_end : unit_begin;
             int prev_h = 0, prev_qb = -1;   // iteration n - 1
             uint32_t n = 0;
-            PairUnit u = {};
+            PairUnit<SINK> u = {};
             int h = 0, h_end = 0, i = 0;
             auto stat = [&](const float* src, int off, int bar, int qb) {
                 mbar_arrive_expect_tx(&bars[bar + (n & 1)], 512);
@@ -291,7 +316,7 @@ k_attn_bwd_pair(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             while (ok) {
                 const bool unit = h == h_end, more = !unit || idx < unit_end;   // the last round only has loads of iteration n - 1
                 if (unit && more) {
-                    u = pair_unit(p, p.cta_tiles[idx++]);
+                    u = pair_unit<SINK>(p, p.cta_tiles[idx++]);
                     h = u.kvh * G;
                     h_end = h + G;
                     i = 0;
@@ -387,7 +412,7 @@ k_attn_bwd_pair(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 }
             };
             for (int idx = unit_begin; idx < unit_end && ok; ++idx) {
-                const PairUnit u = pair_unit(p, p.cta_tiles[idx]);
+                const PairUnit<SINK> u = pair_unit<SINK>(p, p.cta_tiles[idx]);
                 const int n_it = G * u.n_blk;
                 uint32_t begun = 0;              // bit per CTA: its rows of dV and dK have been written
                 if (!wait(L::kKvFull, ucnt)) break;
@@ -459,7 +484,7 @@ k_attn_bwd_pair(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         uint32_t n = 0;
         bool ok = true;
         for (int idx = unit_begin; idx < unit_end && ok; ++idx) {
-            const PairUnit u = pair_unit(p, p.cta_tiles[idx]);
+            const PairUnit<SINK> u = pair_unit<SINK>(p, p.cta_tiles[idx]);
             const int n_it = G * u.n_blk;
             for (int it = 0, i = 0, h = u.kvh * G; it < n_it; ++it, ++n) {
                 const int row = (u.i0 + i) * kBlk + 64 * (int)rank + 32 * (w & 1), head = h;
@@ -496,7 +521,7 @@ k_attn_bwd_pair(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         uint32_t ucnt = 0, n = 0, n_sent = 0;
         bool ok = true;
         for (int idx = unit_begin; idx < unit_end && ok; ++idx) {
-            const PairUnit u = pair_unit(p, p.cta_tiles[idx]);
+            const PairUnit<SINK> u = pair_unit<SINK>(p, p.cta_tiles[idx]);
             const int n_it = G * u.n_blk;
             for (int it = 0; it < n_it && ok; ++it, ++n) {
                 const float* dvec = reinterpret_cast<const float*>(smem + L::kDvecOff + (n & 1) * 512);
@@ -581,12 +606,12 @@ k_attn_bwd_pair(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         bool ok = true;
         for (int idx = unit_begin; idx < unit_end && ok; ++idx) {
             const uint64_t tile_t0 = threadIdx.x == 0 ? globaltimer_ns() : 0;
-            const PairUnit u = pair_unit(p, p.cta_tiles[idx]);
+            const PairUnit<SINK> u = pair_unit<SINK>(p, p.cta_tiles[idx]);
             const int n_it = G * u.n_blk;
             const int64_t k0 = (int64_t)(u.j0 + rank) * kBlk, key = k0 + r;
             const bool key_ok = key < p.T;
             const int kend = key_ok ? p.tok_end[key] : 0;
-            const int min_kend = k0 < p.T ? p.blk[k0 / kBlk].x : 0;
+            const int min_kend = k0 < p.T ? (SINK ? p.blk[k0 / kBlk].x : p.tok_end[k0]) : 0;
             const bool partial = k0 + kBlk > p.T;
             for (int it = 0, i = 0; it < n_it && ok; ++it, ++n) {
                 const int qb = (u.i0 + i) * kBlk;
