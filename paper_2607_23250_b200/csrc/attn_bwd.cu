@@ -1135,6 +1135,7 @@ static int backward(const void* q_dev, const void* k_dev, const void* v_dev, Row
     }
     if (!fused) {
         if (!dq_dir.enabled || !dkv_dir.enabled) return LIBRA_ERR_PLAN_MISMATCH;
+        if (!(plan->asked & LIBRA_DIR_KV) && !(plan->two_kernel && dims->head_dim == 128)) return LIBRA_ERR_PLAN_MISMATCH;   // not the caller's lists
         if (dkv_dir.tile != kBlk || dq_dir.tile != 2 * kBlk) return LIBRA_ERR_UNSUPPORTED;
         if (dkv_dir.H != dims->hkv) return LIBRA_ERR_PLAN_MISMATCH;
         if (dims->hq % dq_dir.H) return LIBRA_ERR_INVALID_ARG;

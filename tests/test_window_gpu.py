@@ -125,6 +125,13 @@ def test_the_form_of_the_backward():
         _check(cu, q, k, v, dout, (out, lse, results[-1][1]), 150, 3)
         plan.destroy()
     assert results[1][0] == results[2][0] < results[0][0]
+    q64, k64, v64, g64 = _tensors(cu, 4, 2, 64, 2)              # as without a window, 64-wide heads need key-major lists
+    plan = _plan(cu, 4, 2, True, 150, 3, n_workers=12)
+    out, lse = lb.libra_attn_pool_fwd(q64, k64, v64, plan)
+    with pytest.raises(lb.LibraError) as err:
+        lb.libra_attn_pool_bwd(q64, k64, v64, out, lse, g64, plan)
+    assert err.value.code == lb.ERR_PLAN_MISMATCH
+    plan.destroy()
     assert all(torch.equal(x, y) for x, y in zip(results[1][1], results[2][1]))
 
 
