@@ -687,7 +687,7 @@ static bool fused_on_pairs(const libra_plan* p, int64_t cells, int64_t wide_cell
 // 700 to 131072 tokens with windows of 32 to 8192 the choice is 1.2 % from the better form on average, always the fused
 // one 12 %, always the other 10 %.
 static bool prefer_two_kernels(const libra_plan* p, bool on_pairs, int64_t cells) {
-    if (!p->window || on_pairs || !p->dir[0].enabled || !p->dir[1].enabled) return false;
+    if (!p->window || on_pairs) return false;
     return cells <= 8 * p->dir[1].NB && 100 * p->dir[1].NT >= (p->sinks ? 135 : 90) * p->W;
 }
 static double heads_per_kv(const libra_plan* p) { return p->dir[0].H > p->dir[2].H ? (double)p->dir[0].H / p->dir[2].H : 1.0; }
@@ -856,17 +856,23 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
         }
     }
     // ---- weights, order, placement and lists of all directions together
+    // Lists that no kernel walks are not made: the key-major ones of a windowed plan whose caller did not ask for them, unless the
+    // two-kernel form was chosen and takes these; with it those of the pair tiles.
+    p->two_kernel = pairs[2] && sorted[0] && sorted[1] && prefer_two_kernels(p, pairs[4], cells);
+    const bool asked = (p->asked & LIBRA_DIR_KV) != 0;
+    const bool live[kDirs] = {sorted[0], sorted[1] && (asked || (p->two_kernel && !p->sinks)), false, sorted[3], false,
+                              sorted[5] && (asked || p->two_kernel), sorted[6]};
     DirViews views = {};
     int n = 0, max_w = 0;
     int64_t max_nb = 0, max_nt = 0;
     for (int k = 0; k < kDirs; ++k)
-        if (sorted[k]) {
+        if (live[k]) {
             views.v[n++] = view_of(p->dir[k], k != 0, o);
             max_nb = p->dir[k].NB > max_nb ? p->dir[k].NB : max_nb;
         }
     if (n > 0) {
-        for (int k = 5, at = n - sorted[5] - sorted[6]; k < kDirs; ++k) {
-            if (!sorted[k]) continue;
+        for (int k = 5, at = n - live[5] - live[6]; k < kDirs; ++k) {
+            if (!live[k]) continue;
             const PlanDir& d = p->dir[k];
             k_tail_units<<<grid_for(d.NB, 256), 256, 0, s>>>(mask, p->d_blk, p->d_blk_near, d.NB - d.n_tails, d.tile, d.tail_rows, d.tail_width,
                                                              views.v[at++]);
@@ -877,11 +883,11 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
         count_launch(2);
     }
     const int n_sorted = n;
-    // No kernel walks the lists of the 128-key pair tiles where the fused backward has its wide ones: they are made when they
-    // are exported.
-    const bool listed[kDirs] = {sorted[0], sorted[1], pairs[2] && !pairs[4], sorted[3] || pairs[3], pairs[4], sorted[5], sorted[6]};
+    // No kernel walks the lists of the 128-key pair tiles where the fused backward has its wide ones, either: they are made when
+    // they are exported.
+    const bool listed[kDirs] = {live[0], live[1], pairs[2] && !pairs[4] && !p->two_kernel, live[3] || pairs[3], pairs[4], live[5], live[6]};
     for (int k = 2; k < kDirs; ++k)
-        if (listed[k] && !sorted[k]) views.v[n++] = view_of(p->dir[k], 1, o);
+        if (listed[k] && !live[k]) views.v[n++] = view_of(p->dir[k], 1, o);
     if (n == 0) return LIBRA_OK;
     for (int k = 0; k < kDirs; ++k)
         if (listed[k]) {
@@ -894,7 +900,7 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
         count_launch();
     }
     for (int k = 0; k < 2; ++k) {   // (not the internal direction, whose tiles are twice as heavy: only its balance would suffer)
-        if (!want[k] || o.weight_model != LIBRA_WEIGHT_BLOCKS) continue;
+        if (!live[k] || o.weight_model != LIBRA_WEIGHT_BLOCKS) continue;
         const DirView v = view_of(p->dir[k], k != 0, o);
         const double chunks = (double)((T + v.g - 1) / v.g);   // at most each of them against all
         if (v.H * chunks * (8 * chunks + v.unit_cost) < 0x1p53) continue;
@@ -902,7 +908,6 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
         count_launch();
     }
     for (int k = 0; k < kDirs; ++k) p->dir[k].enabled = sorted[k] || pairs[k] ? 1 : 0;
-    if (pairs[2]) p->two_kernel = prefer_two_kernels(p, pairs[4], cells);
     return cudaGetLastError() == cudaSuccess ? LIBRA_OK : LIBRA_ERR_CUDA;
 }
 
@@ -1053,7 +1058,7 @@ extern "C" int libra_plan_export(const libra_plan_t* plan, int direction, int64_
     if (weight_host || order_host) ok(cudaMalloc(&tmp, sizeof(int64_t) * (d->NT ? d->NT : 1)));
     if (e != cudaSuccess) return LIBRA_ERR_CUDA;
     // Pair tiles whose lists no kernel walks: made here, the same ones at every call.
-    if (d == &plan->dir[2] && plan->dir[4].enabled && (cta_of_tile_host || cta_offsets_host || cta_tiles_host || loads_host)) {
+    if (d == &plan->dir[2] && (plan->dir[4].enabled || plan->two_kernel) && (cta_of_tile_host || cta_offsets_host || cta_tiles_host || loads_host)) {
         DirViews views = {};
         views.v[0] = view_of(*d, 1, libra_plan_opts{});
         place_lists(views, 1, d->W, d->NT, s);
