@@ -121,6 +121,23 @@ struct FwdTile : FwdTileSinks<SINK> {
     }
     // A tile that a pair of CTAs shares: `shared`, and part[g] when both have key blocks of slot g.
     bool shared, part[2];
+    // Leaves one slot of the tile, as its slot 0; false where it has none.
+    __device__ __forceinline__ bool take_slot(int g) {
+        if constexpr (SINK) {
+            if (g == 1) {
+                if (hi[1] < 0) return false;
+                q0 += kBM;
+                lo[0] = lo[1];
+                hi[0] = hi[1];
+                this->slo[0] = this->slo[1];
+                this->shi[0] = this->shi[1];
+                this->first[0] = this->first[1];
+            }
+            lo[1] = this->slo[1] = 0;
+            hi[1] = this->shi[1] = -1;
+        }
+        return true;
+    }
     // Takes the CTA's part: rank 0 the upper half of the key blocks, rank 1 the lower; false when nothing is left for it.
     __device__ __forceinline__ bool take_half(uint32_t rank) {
         const int top = hi[1] >= 0 ? hi[1] : hi[0], n = top - lo[0] + 1;
@@ -332,7 +349,9 @@ __device__ __noinline__ float2 sink_block(uint8_t* smem, uint64_t* bars, uint32_
 // heads of 64), at the rate of one slot's chain for each, with 84 SMs idle.  Each rank takes
 // the other's maxima, sums and output of the slot of its own number through distributed shared memory and combines: 28.4 ->
 // 21.5 us there, one sample of 4096 tokens, 4 heads of 128: 55.3 -> 38.1.
-template <int D, bool PAIR, bool SINK>
+// SINK: plans with sinks; with SPLIT two CTAs go through a list, one a slot of its tiles.  (An instance of its own: decided at run
+// time, it cost the other one 4 % on 10007 tokens in short samples.)
+template <int D, bool PAIR, bool SINK, bool SPLIT>
 __global__ void __launch_bounds__(kFwdThreads, 1)
 k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
            const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_out, const FwdParams p) {
@@ -358,8 +377,9 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
     const int warp = threadIdx.x >> 5;
     const int lane = threadIdx.x & 31;
     const uint32_t rank = PAIR ? cluster_rank() : 0;
-    const int worker = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
-    const int cta = PAIR ? worker + (int)(rank * (gridDim.x >> 1)) : worker;   // where the CTA reports
+    constexpr bool two = PAIR || SPLIT;   // CTAs for each list
+    const int worker = two ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
+    const int cta = two ? worker + (int)((blockIdx.x & 1) * (gridDim.x >> 1)) : worker;   // where the CTA reports
 
     if (threadIdx.x == 0) {
         mbar_init(bar_spent, 2 * kBM);
@@ -422,6 +442,7 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
             FwdTile<SINK> x;
             while (ok && !(p.inject_stall && (!PAIR || cluster_rank() == 1)) && tiles.next(x)) {
                 if (PAIR && !x.take_half(cluster_rank())) continue;
+                if (SPLIT && !x.take_slot(blockIdx.x & 1)) continue;
                 const bool act1 = x.hi[1] >= 0;
                 const int top = act1 ? x.hi[1] : x.hi[0];
                 for (int hh = 0; hh < heads_per_shard && ok; ++hh) {
@@ -521,6 +542,7 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
             FwdTile<SINK> x;
             while (ok && tiles.next(x)) {
                 if (PAIR && !x.take_half(cluster_rank())) continue;
+                if (SPLIT && !x.take_slot(blockIdx.x & 1)) continue;
                 const bool act1 = x.hi[1] >= 0;
                 const int top = act1 ? x.hi[1] : x.hi[0], last = x.last();
                 for (int hh = 0; hh < heads_per_shard && ok; ++hh) {
@@ -616,6 +638,7 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
         FwdTile<SINK> x;
         while (ok && tiles.next(x)) {
             if (PAIR && !x.take_half(cluster_rank())) continue;
+            if (SPLIT && !x.take_slot(blockIdx.x & 1)) continue;
             const int64_t qs = x.q0 + g * kBM;
             const int lo = x.lo[g], hi = x.hi[g];
             if (lo > hi) {  // slot past the end of the pool, or all in the other CTA
@@ -778,7 +801,7 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
                 // after this group's next P arrival, which follows in program order
                 tc_fence_before();
             }
-            if (threadIdx.x == 0 && ok && (!PAIR || cluster_rank() == 0)) p.tile_ns[x.t] = (uint32_t)(globaltimer_ns() - tile_t0);
+            if (threadIdx.x == 0 && ok && (!two || (blockIdx.x & 1) == 0)) p.tile_ns[x.t] = (uint32_t)(globaltimer_ns() - tile_t0);
         }
         // every bulk store this warp issued has completed before the CTA leaves
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -840,20 +863,20 @@ int make_f32_3d_map(CUtensorMap* m, const void* base, int64_t T, int H, int d, i
     return r == CUDA_SUCCESS ? LIBRA_OK : LIBRA_ERR_CUDA;
 }
 
-template <int D, bool PAIR, bool SINK = false>
+template <int D, bool PAIR, bool SINK = false, bool SPLIT = false>
 static int launch_fwd(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tout,
                       const FwdParams& prm, int W, libra_plan_t* mp, cudaStream_t s) {
     using L = FwdSmem<D>;
-    constexpr int kSlot = (D == 128 ? 0 : 1) + (PAIR ? 5 : (SINK ? 12 : 0));
+    constexpr int kSlot = (D == 128 ? 0 : 1) + (PAIR ? 5 : (SPLIT ? 18 : (SINK ? 12 : 0)));
     if (!cfg_done(kSlot)) {   // per device: the attribute belongs to the device's copy of the kernel
-        if (cudaFuncSetAttribute(k_attn_fwd<D, PAIR, SINK>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kAlloc) != cudaSuccess)
+        if (cudaFuncSetAttribute(k_attn_fwd<D, PAIR, SINK, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kAlloc) != cudaSuccess)
             return LIBRA_ERR_CUDA;
-        if (!regs_pool_ok(k_attn_fwd<D, PAIR, SINK>, 256, LIBRA_FWD_REG_INC, 128, LIBRA_FWD_REG_DEC)) return LIBRA_ERR_UNSUPPORTED;
+        if (!regs_pool_ok(k_attn_fwd<D, PAIR, SINK, SPLIT>, 256, LIBRA_FWD_REG_INC, 128, LIBRA_FWD_REG_DEC)) return LIBRA_ERR_UNSUPPORTED;
         cfg_mark(kSlot);
     }
     count_launch();
-    mp->n_outcome[0] = PAIR ? W / 2 * 2 : W;
-    const cudaError_t e = launch_dependent<PAIR ? 2 : 1>(k_attn_fwd<D, PAIR, SINK>, mp->n_outcome[0], kFwdThreads, L::kAlloc, s,
+    mp->n_outcome[0] = PAIR || SPLIT ? W / 2 * 2 : W;
+    const cudaError_t e = launch_dependent<PAIR ? 2 : 1>(k_attn_fwd<D, PAIR, SINK, SPLIT>, mp->n_outcome[0], kFwdThreads, L::kAlloc, s,
                                                          tq, tk, tv, tout, prm);
     return e == cudaSuccess ? LIBRA_OK : LIBRA_ERR_CUDA;
 }
@@ -921,7 +944,14 @@ extern "C" int libra_attn_pool_fwd(const void* q_dev, const void* k_dev, const v
     // (A window of fewer blocks leaves no tile of kShareBlocks; tiles with sinks are not shared.)
     const bool pair = d.NT <= d.W / 2 && d.H == dims->hq && plan->T >= 4 * kBN * (int64_t)plan->n && plan->sinks == 0 &&
                       (plan->window == 0 || plan->window > (kShareBlocks - 3) * kBN);
-    if (plan->sinks)
+    // Tiles with sinks are not shared by key blocks; where there are two CTAs for each they have a slot each: 4096 tokens, 4 heads
+    // of 64, window 512: 16.2 -> 13.8 us, 2048: 34.1 -> 29.4; 4 / 1 heads of 128, 512: 18.0 -> 15.6; 2000 tokens in samples of up to
+    // 400, 8 / 2 heads, 300: 13.1 -> 12.1.
+    const bool split = plan->sinks && d.NT <= d.W / 2;
+    if (split)
+        rc = dims->head_dim == 128 ? launch_fwd<128, false, true, true>(tq, tk, tv, tout, prm, d.W, mp, s)
+                                   : launch_fwd<64, false, true, true>(tq, tk, tv, tout, prm, d.W, mp, s);
+    else if (plan->sinks)
         rc = dims->head_dim == 128 ? launch_fwd<128, false, true>(tq, tk, tv, tout, prm, d.W, mp, s)
                                    : launch_fwd<64, false, true>(tq, tk, tv, tout, prm, d.W, mp, s);
     else if (dims->head_dim == 128)
