@@ -913,14 +913,16 @@ static int launch_bwd(const CUtensorMap& tq, const CUtensorMap& tk, const CUtens
         if (set_smem(k_attn_bwd_dkdv<D, true, false>, DkvSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
         if (set_smem(k_attn_bwd_dkdv<D, false, true>, DkvSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
         if (set_smem(k_attn_bwd_dkdv<D, true, true>, DkvSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
-        if (set_smem(k_attn_bwd_dq<D, false>, DqSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
-        if (set_smem(k_attn_bwd_dq<D, true>, DqSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
+        if (set_smem(k_attn_bwd_dq<D, false, false>, DqSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
+        if (set_smem(k_attn_bwd_dq<D, true, false>, DqSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
+        if (set_smem(k_attn_bwd_dq<D, true, true>, DqSmem<D>::kBytes) != LIBRA_OK) return LIBRA_ERR_CUDA;
         if (!regs_pool_ok(k_attn_bwd_dkdv<D, false, false>, 128, kDkvRegsDs, 128, kDkvRegsOther)) return LIBRA_ERR_UNSUPPORTED;
         if (!regs_pool_ok(k_attn_bwd_dkdv<D, true, false>, 128, kDkvRegsDs, 128, kDkvRegsOther)) return LIBRA_ERR_UNSUPPORTED;
         if (!regs_pool_ok(k_attn_bwd_dkdv<D, false, true>, 128, kDkvRegsDs, 128, kDkvRegsOther)) return LIBRA_ERR_UNSUPPORTED;
         if (!regs_pool_ok(k_attn_bwd_dkdv<D, true, true>, 128, kDkvRegsDs, 128, kDkvRegsOther)) return LIBRA_ERR_UNSUPPORTED;
-        if (!regs_pool_ok(k_attn_bwd_dq<D, false>, 128 * kDqGroups, kDqRegsCompute, 128, kDqRegsOther)) return LIBRA_ERR_UNSUPPORTED;
-        if (!regs_pool_ok(k_attn_bwd_dq<D, true>, 128 * kDqGroups, kDqRegsCompute, 128, kDqRegsOther)) return LIBRA_ERR_UNSUPPORTED;
+        if (!regs_pool_ok(k_attn_bwd_dq<D, false, false>, 128 * kDqGroups, kDqRegsCompute, 128, kDqRegsOther)) return LIBRA_ERR_UNSUPPORTED;
+        if (!regs_pool_ok(k_attn_bwd_dq<D, true, false>, 128 * kDqGroups, kDqRegsCompute, 128, kDqRegsOther)) return LIBRA_ERR_UNSUPPORTED;
+        if (!regs_pool_ok(k_attn_bwd_dq<D, true, true>, 128 * kDqGroups, kDqRegsCompute, 128, kDqRegsOther)) return LIBRA_ERR_UNSUPPORTED;
         cfg_mark(kSlot);
     }
     time_begin(mp, 1, s);
@@ -928,7 +930,11 @@ static int launch_bwd(const CUtensorMap& tq, const CUtensorMap& tk, const CUtens
     constexpr size_t bytes = DkvSmem<D>::kBytes;
     const unsigned grid = Wa / share * share;
     mp->n_outcome[1] = (int)grid;
-    mp->n_outcome[3] = Wb;
+    // With sinks, and a CTA for each dK/dV tile, the dQ tiles' halves go to two CTAs where there are that many: step's backward of 4096
+    // tokens, 4 / 4 heads of 64, windows 128 / 512 / 2048: 29.1 -> 26.8, 32.2 -> 27.5, 61.7 -> 52.6 us.  Where clusters share the dK/dV
+    // tiles they would only be in each other's way: 4096 tokens, 4 / 1 heads of 128, 512: 44.6 and 52.7.
+    const bool split = mp->sinks && share == 1 && 2 * mp->dir[0].NT <= Wb;
+    mp->n_outcome[3] = split ? Wb / 2 * 2 : Wb;
     auto launch = [&](auto shared, auto alone) {
         switch (share) {
             case 8: return launch_dependent<8>(shared, grid, kBwdThreads, bytes, s, tq, tk, tv, tdo, pa);
@@ -942,8 +948,13 @@ static int launch_bwd(const CUtensorMap& tq, const CUtensorMap& tk, const CUtens
     time_end(mp, 1, s);
     time_begin(mp, 2, s);
     if (e == cudaSuccess)
-        e = mp->sinks ? launch_dependent(k_attn_bwd_dq<D, true>, Wb, kDqThreads, DqSmem<D>::kBytes, s, tq, tk, tv, tdo, tdq, pb)
-                      : launch_dependent(k_attn_bwd_dq<D, false>, Wb, kDqThreads, DqSmem<D>::kBytes, s, tq, tk, tv, tdo, tdq, pb);
+    {
+        auto launch_dq = [&](auto kernel) {
+            return launch_dependent(kernel, mp->n_outcome[3], kDqThreads, DqSmem<D>::kBytes, s, tq, tk, tv, tdo, tdq, pb);
+        };
+        e = split ? launch_dq(k_attn_bwd_dq<D, true, true>)
+                  : (mp->sinks ? launch_dq(k_attn_bwd_dq<D, true, false>) : launch_dq(k_attn_bwd_dq<D, false, false>));
+    }
     time_end(mp, 2, s);
     count_launch(2);
     if (pa.units && e == cudaSuccess) {

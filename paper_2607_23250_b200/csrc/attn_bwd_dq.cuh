@@ -106,14 +106,15 @@ struct DqUnit : DqUnitSinks<SINK> {
         }
     }
 };
-template <bool SINK>
+// SPLIT: two CTAs go through a list, each one 128-row sub-block of its tiles.
+template <bool SINK, bool SPLIT>
 struct DqUnitIter {
     using P = std::conditional_t<SINK, DqSinkParams, DqParams>;
     const P& p;
     int idx, end, sub, hh, hps;
     int t;  // cta_tiles[idx], fetched when idx moves so that the load has a unit's time to land
     __device__ DqUnitIter(const P& p_, int begin, int end_, int heads_per_shard)
-        : p(p_), idx(begin), end(end_), sub(0), hh(0), hps(heads_per_shard) {
+        : p(p_), idx(begin), end(end_), sub(SPLIT ? (int)(blockIdx.x & 1) : 0), hh(0), hps(heads_per_shard) {
         t = idx < end ? p.cta_tiles[idx] : 0;
     }
     __device__ DqUnit<SINK> next() {
@@ -139,8 +140,8 @@ struct DqUnitIter {
             }
             if (!live || ++hh == hps) {
                 hh = 0;
-                if (++sub == 2) {
-                    sub = 0;
+                if (SPLIT || ++sub == 2) {
+                    if (!SPLIT) sub = 0;
                     ++idx;
                     t = idx < end ? p.cta_tiles[idx] : 0;
                 }
@@ -151,11 +152,11 @@ struct DqUnitIter {
     }
 };
 
-template <int D, bool SINK>
+template <int D, bool SINK, bool SPLIT>
 __global__ void __launch_bounds__(kDqThreads, 1)
 k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
               const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_do,
-              const __grid_constant__ CUtensorMap tm_dq, const typename DqUnitIter<SINK>::P p) {
+              const __grid_constant__ CUtensorMap tm_dq, const typename DqUnitIter<SINK, SPLIT>::P p) {
     using L = DqSmem<D>;
     int n_sinks = 0;
     if constexpr (SINK) n_sinks = p.sinks;
@@ -184,7 +185,8 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
 
     const int warp = threadIdx.x >> 5;
     const int lane = threadIdx.x & 31;
-    const int cta = blockIdx.x;
+    const int worker = SPLIT ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
+    const int cta = SPLIT ? worker + (int)((blockIdx.x & 1) * (gridDim.x >> 1)) : worker;   // where the CTA reports
 
     if ((smem_u32(smem) & 1023u) != 0) {
         if (threadIdx.x == 0) p.outcome[cta] = LIBRA_ERR_CUDA;
@@ -239,8 +241,8 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     constexpr uint32_t kColS = 0, kColDP = 128, kColDQ = 256, kColQ = 256 + D, kColDO = 256 + D + D / 2;
     static_assert(kColDO + D / 2 <= 512, "TMEM columns");
 
-    const int tile_begin = p.cta_offsets[cta];
-    const int tile_end = p.cta_offsets[cta + 1];
+    const int tile_begin = p.cta_offsets[worker];
+    const int tile_end = p.cta_offsets[worker + 1];
     const int heads_per_shard = p.hq / p.H;
     const int G = p.hq / p.hkv;
 
@@ -257,7 +259,7 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         // cycles per unit.
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDqRegsOther));
         if (elect_one()) {
-            DqUnitIter<SINK> units(p, tile_begin, tile_end, heads_per_shard);
+            DqUnitIter<SINK, SPLIT> units(p, tile_begin, tile_end, heads_per_shard);
             DqUnit<SINK> u = units.next();
             uint32_t cnt = 0;
             bool ok = true;
@@ -287,7 +289,7 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             uint32_t ucnt = 0, kcnt = 0, vcnt = 0;
             uint32_t n_q = 0, n_do = 0;   // Q / dO loads armed so far (for the give-up path)
             bool ok = true;
-            DqUnitIter<SINK> units(p, tile_begin, tile_end, heads_per_shard);
+            DqUnitIter<SINK, SPLIT> units(p, tile_begin, tile_end, heads_per_shard);
             DqUnit<SINK> u = units.next();
             // Q and dO of unit `un`, whose tiles go through phase `cnt` of their barriers.  The shared-memory
             // copies are free again as soon as the compute groups have moved the previous unit's rows into
@@ -414,7 +416,7 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                 ++vcnt;
                 return true;
             };
-            DqUnitIter<SINK> units(p, tile_begin, tile_end, heads_per_shard);
+            DqUnitIter<SINK, SPLIT> units(p, tile_begin, tile_end, heads_per_shard);
             DqUnit<SINK> u = units.next();
             uint32_t ucnt = 0;
             if (u.valid) {  // first unit: nothing to overlap its first S and dP with
@@ -550,7 +552,7 @@ k_attn_bwd_dq(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             x.dsum = p.dvec[(size_t)un.h * p.Tpad + row];
             return x;
         };
-        DqUnitIter<SINK> units(p, tile_begin, tile_end, heads_per_shard);
+        DqUnitIter<SINK, SPLIT> units(p, tile_begin, tile_end, heads_per_shard);
         DqUnit<SINK> u = units.next();
         RowCtx cx{};
         if (u.valid) {
