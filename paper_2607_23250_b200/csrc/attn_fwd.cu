@@ -746,7 +746,7 @@ k_attn_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
                         x.sink_groups(g, j, p.sinks, c0, c1);
                         const float2 ml = sink_block<D>(smem, bars, t_s, t_o, make_int4(c0, c1, sink_lo - j * kBN, sink_hi - j * kBN), p.scale_log2,
                                                         make_float2(m_ref, l_sum), scnt & 1, (ocnt - 1) & 1);
-                        ok = __all_sync(0xffffffffu, ml.y >= 0.f);
+                        ok = !__any_sync(0xffffffffu, ml.y < 0.f);   // (a NaN sum is a row's own affair)
                         if (!ok) break;
                         ++scnt;
                         ++ocnt;

@@ -330,3 +330,33 @@ def test_values_that_are_not_finite_stay_near(d, fused, value):
     far[:256] = False                                                   # the sinks' tile
     assert same(dk[far], grads[1][far]) and same(dv[far], grads[2][far])
     plan.destroy()
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+@pytest.mark.parametrize("d,T,hq", [(64, 2300, 2), (64, 21000, 6), (128, 2300, 2), (128, 21000, 6), (256, 9000, 4)])
+def test_a_row_without_a_number_ends_no_launch(d, T, hq, value):
+    """Rows that see a key that is not finite are NaN, sinks or not; the worker that met them goes on to its other tiles.  Sizes at
+    which a tile has a CTA for each half (2300), one, and a worker several tiles."""
+    from paper_2607_23250_b200 import binding as lb
+    window, sinks, at = 300, 4, 900
+    cu = pools.cu_seqlens([T])
+    q, k, v, dout = _tensors(cu, hq, 1, d, 6)
+    for fused in (False, True) if d != 64 else (False,):
+        plan = _plan(cu, hq, 1, fused, window, sinks)
+        want, want_lse = lb.libra_attn_pool_fwd(q, k, v, plan)
+        k2 = k.clone()
+        k2[at] = value
+        out, lse = torch.full_like(want, 7.0), torch.full_like(want_lse, 7.0)
+        lb.libra_attn_pool_fwd(q, k2, v, plan, out=out, lse=lse)
+        torch.cuda.synchronize()
+        plan.busy_times(lb.KERNEL_FWD)                                  # raises where a CTA gave up
+        # q has values of either sign in every row: their products with infinities add up to NaN
+        assert out[at:at + window].isnan().all() and lse[:, at:at + window].isnan().all()
+        far = torch.ones(T, dtype=torch.bool, device="cuda")
+        far[at // 256 * 256:(at // 128 * 128 + 127 + window - 1) // 256 * 256 + 256] = False
+        assert torch.equal(out[far], want[far]) and torch.equal(lse[:, far], want_lse[:, far])
+        grads = lb.libra_attn_pool_bwd(q, k2, v, out, lse, dout, plan)
+        torch.cuda.synchronize()
+        plan.busy_times(lb.KERNEL_BWD_FUSED if fused and d == 128 and plan.fused_ctas() > 0 else lb.KERNEL_BWD_DQ)
+        assert grads[0][at:at + window].isnan().all()
+        plan.destroy()
