@@ -893,8 +893,12 @@ static BwdWorkspace bwd_workspace(int64_t T, int hq, int hkv, int d, bool fused,
 }
 // A plan with pair tiles selects the accumulating forms: at head_dim 128 the fused kernel (dQ, dK, dV accumulated in
 // fp32), at head_dim 256 the dV and dK passes over pair tiles (dK, dV accumulated in fp32; the dQ pass is unchanged).
+// The fused form does not walk the query-major lists: where their head shards do not divide the heads, it is the form that runs.
+static bool two_kernels_chosen(const libra_plan_t* plan, const libra_dims* dims) {
+    return plan->two_kernel && dims->hq % plan->dir[0].H == 0;
+}
 static bool use_fused(const libra_plan_t* plan, const libra_dims* dims) {
-    return plan->dir[2].enabled && ((dims->head_dim == 128 && !plan->two_kernel) || dims->head_dim == 256);
+    return plan->dir[2].enabled && ((dims->head_dim == 128 && !two_kernels_chosen(plan, dims)) || dims->head_dim == 256);
 }
 
 template <typename Kernel>
@@ -1021,6 +1025,7 @@ static int launch_fused(const void* q_dev, const void* k_dev, const void* v_dev,
     const int64_t T = plan->T;
     if (d.tile != kBlk || d.H != dims->hkv) return LIBRA_ERR_PLAN_MISMATCH;
     if (d.W > plan->sm_count) return LIBRA_ERR_UNSUPPORTED;
+    if (plan->two_kernel && list_pair_tiles(plan, s) != cudaSuccess) return LIBRA_ERR_CUDA;
     float* dvec = reinterpret_cast<float*>(ws_dev);
     float* lse2 = reinterpret_cast<float*>(ws_dev + ws.stat_bytes);
     float* dq_acc = reinterpret_cast<float*>(ws_dev + 2 * ws.stat_bytes);
@@ -1146,7 +1151,7 @@ static int backward(const void* q_dev, const void* k_dev, const void* v_dev, Row
     }
     if (!fused) {
         if (!dq_dir.enabled || !dkv_dir.enabled) return LIBRA_ERR_PLAN_MISMATCH;
-        if (!(plan->asked & LIBRA_DIR_KV) && !(plan->two_kernel && dims->head_dim == 128)) return LIBRA_ERR_PLAN_MISMATCH;   // not the caller's lists
+        if (!(plan->asked & LIBRA_DIR_KV) && !(two_kernels_chosen(plan, dims) && dims->head_dim == 128)) return LIBRA_ERR_PLAN_MISMATCH;   // not the caller's lists
         if (dkv_dir.tile != kBlk || dq_dir.tile != 2 * kBlk) return LIBRA_ERR_UNSUPPORTED;
         if (dkv_dir.H != dims->hkv) return LIBRA_ERR_PLAN_MISMATCH;
         if (dims->hq % dq_dir.H) return LIBRA_ERR_INVALID_ARG;

@@ -96,6 +96,8 @@ constexpr int kMaxDevices = 64;
 constexpr int kCfgSlots = 24;
 bool cfg_done(int slot);
 void cfg_mark(int slot);
+// Makes the lists of direction 2 where planning has left them out (two_kernel, or direction 4 there), the same ones at every call.
+cudaError_t list_pair_tiles(const libra_plan* plan, cudaStream_t s);
 // LIBRA_ERR_PLAN_MISMATCH when the current device is not the one the plan was built on.
 int check_plan_device(const libra_plan* plan);
 // Kernel timing (libra_plan_set_timing): events on the launch stream around kernel k (LIBRA_KERNEL_* - 1).

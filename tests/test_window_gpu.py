@@ -135,6 +135,30 @@ def test_the_form_of_the_backward():
     assert all(torch.equal(x, y) for x, y in zip(results[1][1], results[2][1]))
 
 
+@pytest.mark.parametrize("sinks", [0, 3])
+@pytest.mark.parametrize("heads,tile", [(4, 128), (3, 256), (4, 384)])
+def test_plans_that_only_the_fused_form_can_take(heads, tile, sinks):
+    """A pool for which the two-kernel form would be the faster one, but whose query-major lists its kernels cannot walk: tiles of
+    another size, head shards that do not divide the heads.  The fused form needs neither."""
+    from paper_2607_23250_b200 import binding as lb
+    cu = pools.cu_seqlens([900, 300])
+    q, k, v, dout = _tensors(cu, 4, 2, 128, 2)
+    first = _plan(cu, 4, 2, True, 150, sinks, n_workers=12)
+    assert first.fused_ctas() == 0
+    out, lse = lb.libra_attn_pool_fwd(q, k, v, first)
+    plan = lb.libra_plan_tiles(torch.from_numpy(cu).cuda(), heads, tile, directions=lb.LIBRA_DIR_Q | lb.LIBRA_DIR_PAIR, tile_kv=128,
+                               n_heads_kv=2, window=150, sinks=sinks, n_workers=12)
+    assert plan.status() == 0 and plan.fused_ctas() == (1 if tile != 256 else 0)
+    assert (lb.libra_attn_pool_bwd_workspace_bytes(plan, q, k) > lb.libra_attn_pool_bwd_workspace_bytes(first, q, k))
+    for _ in range(2):
+        grads = lb.libra_attn_pool_bwd(q, k, v, out, lse, dout, plan)
+        torch.cuda.synchronize()
+        plan.busy_times(lb.KERNEL_BWD_FUSED)
+        _check(cu, q, k, v, dout, (out, lse, grads), 150, sinks)
+    first.destroy()
+    plan.destroy()
+
+
 @pytest.mark.parametrize("d,fused", FORMS)
 def test_a_window_that_reaches_everything_changes_nothing(d, fused):
     from paper_2607_23250_b200 import binding as lb
