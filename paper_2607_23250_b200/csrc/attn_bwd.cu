@@ -1240,7 +1240,7 @@ static int backward(const void* q_dev, const void* k_dev, const void* v_dev, Row
     pa.dv = reinterpret_cast<__nv_bfloat16*>(dv_dev);
     pa.lse2 = lse2;
     pa.dvec = dvec;
-    const PlanDir& dkv_lists = plan->sinks ? plan->dir[5] : dkv_dir;
+    const PlanDir& dkv_lists = plan->dir[5].enabled ? plan->dir[5] : dkv_dir;
     pa.cta_offsets = dkv_lists.d_cta_offsets;
     pa.cta_tiles = dkv_lists.d_cta_exec;
     pa.units = dkv_lists.d_units;

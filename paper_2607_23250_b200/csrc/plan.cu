@@ -756,7 +756,8 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
     const int64_t T = p->T;
     cudaStream_t s = p->stream;
     const bool wide_pairs = want[3] && want[2];                   // the wide tiles are pair tiles
-    const bool sorted[kDirs] = {want[0], want[1], false, want[3] && !want[2], false, want[5], want[6]};   // sizes known, placed heaviest first
+    bool sorted[kDirs] = {want[0], want[1], false, want[3] && !want[2], false, want[5], want[6]};   // sizes known, placed heaviest first
+    const bool asked_kv = (p->asked & LIBRA_DIR_KV) != 0;
     bool pairs[kDirs] = {false, false, want[2], wide_pairs, want[4], false, false};
     for (int k = 0; k < kDirs; ++k) {
         if (!sorted[k]) continue;
@@ -779,8 +780,17 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
             d.n_tails = (int)((NRB + R - 1) / R * width);
             d.NB += d.n_tails;
         }
-        if (const int rc = check_dir(p, p->dir[k], false); rc != LIBRA_OK) return rc;
+        if (const int rc = check_dir(p, p->dir[k], false); rc != LIBRA_OK) {
+            // Lists of the library's own that would be too long are left out: the backward is then the fused one (not asked for
+            // key-major lists), or goes through whole key blocks (asked).
+            const bool own = k >= 5 || (k == 1 && !asked_kv);
+            if (!own) return rc;
+            sorted[k] = false;
+            p->dir[k].NB = p->dir[k].NT = 0;
+            p->dir[k].n_tails = p->dir[k].tail_width = 0;
+        }
     }
+    if (!sorted[1]) sorted[5] = sorted[6] = false;
     PairCands cands;
     PairTables chosen[kDirs];
     int64_t* d_totals = nullptr;
@@ -867,10 +877,9 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
     // ---- weights, order, placement and lists of all directions together
     // Lists that no kernel walks are not made: the key-major ones of a windowed plan whose caller did not ask for them, unless the
     // two-kernel form was chosen and takes these; with it those of the pair tiles.
-    p->two_kernel = pairs[2] && sorted[0] && sorted[1] && prefer_two_kernels(p, pairs[4], cells);
-    const bool asked = (p->asked & LIBRA_DIR_KV) != 0;
-    const bool live[kDirs] = {sorted[0], sorted[1] && (asked || (p->two_kernel && !p->sinks)), false, sorted[3], false,
-                              sorted[5] && (asked || p->two_kernel), sorted[6]};
+    p->two_kernel = pairs[2] && sorted[0] && sorted[1] && (!p->sinks || sorted[5]) && prefer_two_kernels(p, pairs[4], cells);
+    const bool live[kDirs] = {sorted[0], sorted[1] && (asked_kv || (p->two_kernel && !p->sinks)), false, sorted[3], false,
+                              sorted[5] && (asked_kv || p->two_kernel), sorted[6]};
     DirViews views = {};
     int n = 0, max_w = 0;
     int64_t max_nb = 0, max_nt = 0;

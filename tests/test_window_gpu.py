@@ -159,6 +159,40 @@ def test_plans_that_only_the_fused_form_can_take(heads, tile, sinks):
     plan.destroy()
 
 
+@pytest.mark.parametrize("sinks", [0, 4])
+def test_plans_of_more_key_blocks_than_the_rank_sort_takes(sinks):
+    """65536 key blocks are the most of a key-major list that is asked for; lists of the library's own stay away from longer ones."""
+    from paper_2607_23250_b200 import binding as lb
+    T = 9_000_000
+    cu = torch.arange(0, T + 1, 4500, dtype=torch.int32).cuda()
+    plan = lb.libra_plan_tiles(cu, 1, 256, directions=lb.LIBRA_DIR_Q | lb.LIBRA_DIR_PAIR, tile_kv=128, window=100, sinks=sinks)
+    assert plan.status() == 0 and plan.fused_ctas() > 0
+    plan.destroy()
+    with pytest.raises(lb.LibraError) as err:
+        lb.libra_plan_tiles(cu, 1, 256, directions=lb.LIBRA_DIR_Q | lb.LIBRA_DIR_KV, tile_kv=128, window=100, sinks=sinks)
+    assert err.value.code == lb.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("window,sinks", [(300, 4), (1500, 200)])
+def test_the_longest_pool_of_the_two_kernel_form(window, sinks):
+    """65536 key blocks with sinks (no room for lists in which their tails are tiles of their own): 2048 copies of a sample, each of
+    which has the gradients of the first, bit for bit."""
+    from paper_2607_23250_b200 import binding as lb
+    n, copies = 4096, 2048
+    t = pools.make_tensors(n, 1, 1, 64, seed=window, device="cuda")
+    small = [t[x] for x in ("q", "k", "v", "dout")]
+    q, k, v, dout = (x.repeat(copies, 1, 1) for x in small)
+    cu = np.arange(0, n * copies + 1, n, dtype=np.int32)
+    plan = _plan(cu, 1, 1, False, window, sinks)
+    got = _run(plan, q, k, v, dout, False)
+    one = (got[0][:n], got[1][:, :n], [g[:n] for g in got[2]])
+    _check(np.array([0, n], np.int32), *small, one, window, sinks)
+    assert torch.equal(got[0].view(copies, n, 64), one[0].view(1, n, 64).expand(copies, n, 64))
+    for g, first in zip(got[2], one[2]):
+        assert torch.equal(g.view(copies, n, 64), first.view(1, n, 64).expand(copies, n, 64))
+    plan.destroy()
+
+
 @pytest.mark.parametrize("d,fused", FORMS)
 def test_a_window_that_reaches_everything_changes_nothing(d, fused):
     from paper_2607_23250_b200 import binding as lb
