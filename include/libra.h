@@ -218,7 +218,9 @@ int libra_attn_pool_fwd(const void* q_dev, const void* k_dev, const void* v_dev,
                         void* out_dev, float* lse_dev, const libra_dims* dims, void* stream);
 
 /* Bytes of caller-owned device scratch libra_attn_pool_bwd needs; 0 on bad arguments.  Two-kernel form: the row
- * statistics D and LSE in log2 units, padded to a multiple of 128 rows (2 * hq * round_up(T, 128) floats).
+ * statistics D and LSE in log2 units, padded to a multiple of 128 rows (2 * hq * round_up(T, 128) floats); with sinks
+ * (libra_plan_tiles_window) in addition the partial sums of dK and dV of key blocks that hold sinks, as many as the plan's
+ * length, window, sinks and workers make of them.
  * Fused form (see below): in addition the fp32 accumulators of dQ (T * hq * 128 floats) and of dK and dV
  * (T * hkv * 128 floats each). */
 size_t libra_attn_pool_bwd_workspace_bytes(const libra_plan_t* plan, const libra_dims* dims);
@@ -270,7 +272,10 @@ int libra_attn_pool_bwd(const void* q_dev, const void* k_dev, const void* v_dev,
  * start-up.  The call performs no cudaMalloc / cudaFree and calls no allocating routine.
  *   - Limit: libra_attn_pool_bwd_workspace_bytes(plan, dims) must not exceed the built-in size
  *     (2 * hq * round_up(T, 128) floats <= 4 Mi floats); otherwise nothing is launched and
- *     LIBRA_ERR_SCRATCH_TOO_SMALL is returned.
+ *     LIBRA_ERR_SCRATCH_TOO_SMALL is returned.  A plan with sinks has the same limit as long as it was made with
+ *     LIBRA_DIR_KV and takes the two-kernel form: where its partial sums do not fit, key blocks that hold sinks are walked
+ *     whole, which adds the same terms in another order (run-to-run identical, and equal to libra_attn_pool_bwd to
+ *     rounding) and takes longer where samples are long.
  *   - The first call on each device looks up the array's device address (with that device
  *     current); make that first call outside any stream capture.
  *   - All calls on a device share the one array and it keeps the previous call's contents; the

@@ -1005,11 +1005,22 @@ static cudaError_t launch_prep(const RowsOut& out, const void* dout, const float
 using namespace libra;
 
 
+// Tail tiles that a call cuts off the sinks' key blocks; none where it walks whole ones (tails false, or no such lists).
+static int tails_of(const libra_plan_t* plan, const libra_dims* dims, bool tails) {
+    return tails ? plan->dir[dims->head_dim == 256 ? 6 : 5].n_tails : 0;
+}
+
+namespace libra {
+size_t bwd_bytes(const libra_plan_t* plan, const libra_dims* dims, bool tails) {
+    return bwd_workspace(plan->T, dims->hq, dims->hkv, dims->head_dim, use_fused(plan, dims), tails_of(plan, dims, tails)).total;
+}
+}  // namespace libra
+
 extern "C" size_t libra_attn_pool_bwd_workspace_bytes(const libra_plan_t* plan, const libra_dims* dims) {
     if (!plan || !dims || dims->hq <= 0 || dims->hkv <= 0 ||
         (dims->head_dim != 64 && dims->head_dim != 128 && dims->head_dim != 256))
         return 0;
-    return bwd_workspace(plan->T, dims->hq, dims->hkv, dims->head_dim, use_fused(plan, dims), plan->dir[dims->head_dim == 256 ? 6 : 5].n_tails).total;
+    return bwd_bytes(plan, dims, true);
 }
 
 // fp32 tensor [T, H, 128] viewed as (128, H, T); box = 32 floats x 1 head x 32 rows, 128-byte swizzle.
@@ -1133,10 +1144,10 @@ static RestoredQkv restored_qkv(size_t own, const libra_dims* dims) {
     return r;
 }
 
-// held: q, k, v and out come from a checkpoint, q_dev, k_dev and v_dev are null.
+// held: q, k, v and out come from a checkpoint, q_dev, k_dev and v_dev are null.  tails: see bwd_bytes.
 static int backward(const void* q_dev, const void* k_dev, const void* v_dev, RowsOut out, const float* lse_dev,
                     const void* dout_dev, const libra_plan_t* plan, void* dq_dev, void* dk_dev, void* dv_dev, void* workspace_dev,
-                    const libra_dims* dims, void* stream) {
+                    const libra_dims* dims, bool tails, void* stream) {
     if (dims->hq <= 0 || dims->hkv <= 0 || dims->hq % dims->hkv) return LIBRA_ERR_INVALID_ARG;
     if (dims->head_dim != 64 && dims->head_dim != 128 && dims->head_dim != 256) return LIBRA_ERR_UNSUPPORTED;
     const PlanDir& dq_dir = plan->dir[0];
@@ -1167,7 +1178,7 @@ static int backward(const void* q_dev, const void* k_dev, const void* v_dev, Row
 
     const int D = dims->head_dim;
     const int64_t T = plan->T;
-    const BwdWorkspace ws = bwd_workspace(T, dims->hq, dims->hkv, D, fused, plan->dir[D == 256 ? 6 : 5].n_tails);
+    const BwdWorkspace ws = bwd_workspace(T, dims->hq, dims->hkv, D, fused, tails_of(plan, dims, tails));
     float* dvec = reinterpret_cast<float*>(workspace_dev);
     float* lse2 = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace_dev) + ws.stat_bytes);
     cudaStream_t s = (cudaStream_t)stream;
@@ -1196,10 +1207,11 @@ static int backward(const void* q_dev, const void* k_dev, const void* v_dev, Row
         time_end(mp256, 3, s);
         if (e256 != cudaSuccess) return LIBRA_ERR_CUDA;
         mp256->bwd_mask = 2 | 4 | 8;
-        float* partial = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace_dev) + 2 * ws.stat_bytes);
+        float* partial = !fused && tails && plan->dir[6].enabled
+                             ? reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace_dev) + 2 * ws.stat_bytes) : nullptr;
         int rc256 = launch_bwd_d256(q_dev, k_dev, v_dev, dout_dev, dq_dev, dk_dev, dv_dev, lse2, dvec, ws.Tpad, dk_acc,
                                     dv_acc, partial, plan, dims, scale, s);
-        if (rc256 == LIBRA_OK && !fused && plan->dir[6].enabled) {
+        if (rc256 == LIBRA_OK && partial) {
             time_begin(mp256, 5, s);
             if (launch_sum_tails<256>(plan, plan->dir[6], partial, dims->hkv, scale, dk_dev, dv_dev, s) != cudaSuccess) rc256 = LIBRA_ERR_CUDA;
             time_end(mp256, 5, s);
@@ -1240,7 +1252,7 @@ static int backward(const void* q_dev, const void* k_dev, const void* v_dev, Row
     pa.dv = reinterpret_cast<__nv_bfloat16*>(dv_dev);
     pa.lse2 = lse2;
     pa.dvec = dvec;
-    const PlanDir& dkv_lists = plan->dir[5].enabled ? plan->dir[5] : dkv_dir;
+    const PlanDir& dkv_lists = tails && plan->dir[5].enabled ? plan->dir[5] : dkv_dir;
     pa.cta_offsets = dkv_lists.d_cta_offsets;
     pa.cta_tiles = dkv_lists.d_cta_exec;
     pa.units = dkv_lists.d_units;
@@ -1294,14 +1306,23 @@ static int backward(const void* q_dev, const void* k_dev, const void* v_dev, Row
                     : launch_bwd<64>(tq, tk, tv, tdo, tdq, pa, dkv_dir.W, share, pb, dq_dir.W, mp, s);
 }
 
+namespace libra {
+int attn_pool_bwd(const void* q_dev, const void* k_dev, const void* v_dev, const void* out_dev, const float* lse_dev, const void* dout_dev,
+                  const int32_t* cu_seqlens_dev, const libra_plan_t* plan, void* dq_dev, void* dk_dev, void* dv_dev, void* workspace_dev,
+                  const libra_dims* dims, bool tails, void* stream) {
+    if (!q_dev || !k_dev || !v_dev || !out_dev || !lse_dev || !dout_dev || !cu_seqlens_dev || !plan || !dq_dev ||
+        !dk_dev || !dv_dev || !workspace_dev || !dims)
+        return LIBRA_ERR_INVALID_ARG;
+    return backward(q_dev, k_dev, v_dev, {out_dev, nullptr, {}}, lse_dev, dout_dev, plan, dq_dev, dk_dev, dv_dev, workspace_dev, dims, tails, stream);
+}
+}  // namespace libra
+
 extern "C" int libra_attn_pool_bwd(const void* q_dev, const void* k_dev, const void* v_dev, const void* out_dev,
                                    const float* lse_dev, const void* dout_dev, const int32_t* cu_seqlens_dev,
                                    const libra_plan_t* plan, void* dq_dev, void* dk_dev, void* dv_dev,
                                    void* workspace_dev, const libra_dims* dims, void* stream) {
-    if (!q_dev || !k_dev || !v_dev || !out_dev || !lse_dev || !dout_dev || !cu_seqlens_dev || !plan || !dq_dev ||
-        !dk_dev || !dv_dev || !workspace_dev || !dims)
-        return LIBRA_ERR_INVALID_ARG;
-    return backward(q_dev, k_dev, v_dev, {out_dev, nullptr, {}}, lse_dev, dout_dev, plan, dq_dev, dk_dev, dv_dev, workspace_dev, dims, stream);
+    return attn_pool_bwd(q_dev, k_dev, v_dev, out_dev, lse_dev, dout_dev, cu_seqlens_dev, plan, dq_dev, dk_dev, dv_dev, workspace_dev, dims, true,
+                         stream);
 }
 
 extern "C" size_t libra_attn_pool_bwd_ckpt8_workspace_bytes(const libra_plan_t* plan, const libra_dims* dims) {
@@ -1316,5 +1337,5 @@ extern "C" int libra_attn_pool_bwd_ckpt8(const libra_ckpt8* ckpt, const float* l
         return LIBRA_ERR_INVALID_ARG;
     if (!ckpt->q || !ckpt->k || !ckpt->v || !ckpt->out || !ckpt->q_exp || !ckpt->k_exp || !ckpt->v_exp || !ckpt->out_exp)
         return LIBRA_ERR_INVALID_ARG;
-    return backward(nullptr, nullptr, nullptr, {nullptr, ckpt, {}}, lse_dev, dout_dev, plan, dq_dev, dk_dev, dv_dev, workspace_dev, dims, stream);
+    return backward(nullptr, nullptr, nullptr, {nullptr, ckpt, {}}, lse_dev, dout_dev, plan, dq_dev, dk_dev, dv_dev, workspace_dev, dims, true, stream);
 }

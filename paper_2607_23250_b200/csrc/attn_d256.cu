@@ -924,7 +924,7 @@ int launch_bwd_d256(const void* q, const void* k, const void* v, const void* dou
     using namespace d256;
     const PlanDir& dq_dir = plan->dir[0];
     const bool pairs = dk_acc != nullptr;            // key-stationary passes over pair tiles, fp32 accumulators
-    const bool tails = !pairs && plan->dir[6].enabled;
+    const bool tails = partial != nullptr;
     const PlanDir& kv_dir = plan->dir[tails ? 6 : 3];   // 256 keys a tile, in pair tiles or key-major
     if (!kv_dir.enabled || (kv_dir.d_u_blk != nullptr) != pairs) return LIBRA_ERR_PLAN_MISMATCH;
     // whole 128-row tiles (stationary), halves of a streamed block's rows (32) and of its columns (64-row boxes)

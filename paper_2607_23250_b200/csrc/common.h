@@ -128,9 +128,15 @@ int make_f32_3d_map(CUtensorMap* m, const void* base, int64_t T, int H, int d, i
 // its key-major (dV, dK) and query-major (dQ) lists, given the row statistics lse2 / dvec [Hq, Tpad].
 int launch_fwd_d256(const void* q, const void* k, const void* v, void* out, float* lse, const libra_plan* plan,
                     const libra_dims* dims, float scale, cudaStream_t s);
+// libra_attn_pool_bwd and its workspace with the choice whether the sinks' tails are tiles of their own, which takes room for their
+// partial sums; without them the two-kernel form walks the key-major lists of whole key blocks, which are there when the
+// caller has asked for that direction.
+size_t bwd_bytes(const libra_plan_t* plan, const libra_dims* dims, bool tails);
+int attn_pool_bwd(const void* q, const void* k, const void* v, const void* out, const float* lse, const void* dout, const int32_t* cu_seqlens,
+                  const libra_plan_t* plan, void* dq, void* dk, void* dv, void* workspace, const libra_dims* dims, bool tails, void* stream);
 // dk_acc / dv_acc: fp32 accumulators [T, Hkv, 256], zero on entry, when the dV and dK passes are to walk the plan's
 // pair tiles (the caller rounds them afterwards); null: key-major tiles, dk / dv written directly.
-// partial: slots of partial sums, for plans with direction 6 (the caller adds them up).
+// partial: slots of partial sums, for the lists of direction 6 (the caller adds them up); null: whole key blocks.
 int launch_bwd_d256(const void* q, const void* k, const void* v, const void* dout, void* dq, void* dk, void* dv,
                     const float* lse2, const float* dvec, int64_t Tpad, float* dk_acc, float* dv_acc, float* partial,
                     const libra_plan* plan, const libra_dims* dims, float scale, cudaStream_t s);

@@ -11,7 +11,8 @@
 
 namespace {
 
-// Scratch for the two row statistics, D_i and LSE in log2 units: 2 x hq x round_up(T, 128) floats.
+// Scratch for the two row statistics, D_i and LSE in log2 units: 2 x hq x round_up(T, 128) floats, and for the partial sums of
+// plans with sinks where there is room for those, too.
 // 4 Mi floats = 16 MiB, enough for e.g. 32 query heads x 65536 tokens.  Every GPU whose context
 // loads this library holds the array until the process exits.
 constexpr size_t kMaxScratchFloats = size_t(4) << 20;
@@ -49,14 +50,22 @@ extern "C" int libra_attn_pool_bwd_noalloc(const void* q_dev, const void* k_dev,
     // the same verdicts, in the same order, as the regular entry point gives for bad dimensions
     if (dims->hq <= 0 || dims->hkv <= 0 || dims->hq % dims->hkv) return LIBRA_ERR_INVALID_ARG;
     if (dims->head_dim != 64 && dims->head_dim != 128 && dims->head_dim != 256) return LIBRA_ERR_UNSUPPORTED;
-    const size_t need = libra_attn_pool_bwd_workspace_bytes(plan, dims);
+    size_t need = libra_attn_pool_bwd_workspace_bytes(plan, dims);
     if (need == 0) return LIBRA_ERR_INVALID_ARG;
+    // Partial sums of the sinks' tails are 256 KB a tail and kv head at head_dim 128 (32 / 8 heads, window 1024: 3072 tokens would be the
+    // most).  Beyond that the key-major tiles are walked whole: the same additions in another order, and the tile of a key
+    // block that holds sinks as long as its sample.
+    bool tails = true;
+    if (need > kMaxScratchFloats * sizeof(float) && (plan->asked & LIBRA_DIR_KV)) {
+        tails = false;
+        need = libra::bwd_bytes(plan, dims, false);
+    }
     if (need > kMaxScratchFloats * sizeof(float)) return LIBRA_ERR_SCRATCH_TOO_SMALL;
     void* scratch = nullptr;
     const int rc = scratch_address(&scratch);
     if (rc != LIBRA_OK) return rc;
     // Nothing in the scratch has to start at zero: the row-statistics kernel writes every element the
     // later kernels read, so whatever the previous call left behind is simply overwritten.
-    return libra_attn_pool_bwd(q_dev, k_dev, v_dev, out_dev, lse_dev, dout_dev, cu_seqlens_dev, plan, dq_dev, dk_dev,
-                               dv_dev, scratch, dims, stream);
+    return libra::attn_pool_bwd(q_dev, k_dev, v_dev, out_dev, lse_dev, dout_dev, cu_seqlens_dev, plan, dq_dev, dk_dev,
+                                dv_dev, scratch, dims, tails, stream);
 }

@@ -328,6 +328,46 @@ def test_noalloc_backward_follows_the_plan():
     plan.destroy()
 
 
+@pytest.mark.parametrize("d,sinks,room", [(64, 4, True), (64, 600, False), (128, 4, False), (128, 600, False), (256, 4, False), (256, 600, False)])
+def test_noalloc_backward_without_room_for_the_tails(d, sinks, room):
+    """The limit of the allocation-free call is that of the row statistics, whatever the partial sums of a plan with sinks would
+    take: with room for them the bits of the other call, without it whole key blocks, twice the same bits."""
+    from paper_2607_23250_b200 import binding as lb
+    cu = pools.cu_seqlens([2300, 300])
+    q, k, v, dout = _tensors(cu, 8, 8, d, 4)
+    plan = _plan(cu, 8, 8, False, 100, sinks)
+    limit = lb.libra_attn_pool_bwd_noalloc_max_bytes()
+    assert (lb.libra_attn_pool_bwd_workspace_bytes(plan, q, k) <= limit) == room
+    out, lse, grads = _run(plan, q, k, v, dout, False)
+    mine = [[torch.full_like(x, 7.0) for x in (q, k, v)] for _ in range(2)]
+    for m in mine:
+        lb.libra_attn_pool_bwd_noalloc(q, k, v, out, lse, dout, plan, *m)
+    torch.cuda.synchronize()
+    for kern in (lb.KERNEL_BWD_DKDV, lb.KERNEL_BWD_DQ):
+        plan.busy_times(kern)
+    _check(cu, q, k, v, dout, (out, lse, mine[0]), 100, sinks)
+    assert all(torch.equal(x, y) for x, y in zip(*mine))
+    assert torch.equal(grads[0], mine[0][0])
+    if room:
+        assert all(torch.equal(x, y) for x, y in zip(grads, mine[0]))
+    plan.destroy()
+
+
+def test_noalloc_backward_refuses_what_only_the_tails_lists_can_do():
+    """A plan whose key-major lists are the library's own has no lists of whole key blocks."""
+    from paper_2607_23250_b200 import binding as lb
+    cu = pools.cu_seqlens([2300, 300])
+    q, k, v, dout = _tensors(cu, 8, 8, 128, 4)
+    plan = _plan(cu, 8, 8, True, 100, 300, n_workers=12)
+    assert plan.fused_ctas() == 0
+    out, lse = lb.libra_attn_pool_fwd(q, k, v, plan)
+    launches = lb.launch_count()
+    with pytest.raises(lb.LibraError) as err:
+        lb.libra_attn_pool_bwd_noalloc(q, k, v, out, lse, dout, plan, *[torch.empty_like(x) for x in (q, k, v)])
+    assert err.value.code == lb.ERR_SCRATCH_TOO_SMALL and lb.launch_count() == launches
+    plan.destroy()
+
+
 @pytest.mark.parametrize("d", [64, 128, 256])
 def test_stalled_producers_give_up_cleanly(d):
     """The bounded waits of the kernels with sinks, as in the tests of the others: no loads are issued, the launch reports a
