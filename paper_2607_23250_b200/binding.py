@@ -223,13 +223,45 @@ def _chk(*ts):
         assert t.is_cuda and t.is_contiguous(), "expected contiguous CUDA tensors"
 
 
-def libra_attn_pool_fwd(q, k, v, plan: Plan, out=None, lse=None, scale=None, stream=None):
-    """out [T,Hq,d] bf16, lse [Hq,T] fp32 (allocated with torch when not given)."""
+def _chk_qkv(q, k, v):
     _chk(q, k, v)
     assert q.dtype == k.dtype == v.dtype == torch.bfloat16
     T, hq, d = q.shape
+    assert k.shape == v.shape and k.shape[0] == T and k.shape[2] == d, "shapes of q, k and v do not match"
+    assert k.device == v.device == q.device, "tensors on different devices"
+    return T, hq, d
+
+
+def _given(what, t, n, dtype, like):
+    """A tensor of n values that the kernels read or write as a whole."""
+    assert t.dtype is dtype and t.numel() == n, f"{what}: expected {n} values of {dtype}, not {t.numel()} of {t.dtype}"
+    assert t.is_cuda and t.is_contiguous() and t.device == like.device, f"{what}: expected a contiguous tensor on {like.device}"
+
+
+def _workspace(workspace, need, like):
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=like.device)
+    assert workspace.is_cuda and workspace.is_contiguous() and workspace.device == like.device
+    size = workspace.numel() * workspace.element_size()
+    assert size >= need, f"workspace of {size} bytes, the call needs {need}"
+    return workspace
+
+
+def _chk_bwd(q, k, v, out, lse, dout, dq, dk, dv):
+    T, hq, _ = _chk_qkv(q, k, v)
+    n, n_kv = q.numel(), k.numel()
+    _given("lse", lse, hq * T, torch.float32, q)
+    for what, t, size in (("out", out, n), ("dout", dout, n), ("dq", dq, n), ("dk", dk, n_kv), ("dv", dv, n_kv)):
+        _given(what, t, size, torch.bfloat16, q)
+
+
+def libra_attn_pool_fwd(q, k, v, plan: Plan, out=None, lse=None, scale=None, stream=None):
+    """out [T,Hq,d] bf16, lse [Hq,T] fp32 (allocated with torch when not given)."""
+    T, hq, _ = _chk_qkv(q, k, v)
     out = torch.empty_like(q) if out is None else out
     lse = torch.empty((hq, T), dtype=torch.float32, device=q.device) if lse is None else lse
+    _given("out", out, q.numel(), torch.bfloat16, q)
+    _given("lse", lse, hq * T, torch.float32, q)
     dims = _dims(q, k, plan, scale)
     _check(_lib.libra_attn_pool_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(plan.cu_seqlens), plan._h, _ptr(out), _ptr(lse),
                                     ctypes.byref(dims), _stream(stream)), "libra_attn_pool_fwd")
@@ -243,12 +275,13 @@ def libra_attn_pool_bwd_workspace_bytes(plan: Plan, q, k) -> int:
 
 def libra_attn_pool_bwd(q, k, v, out, lse, dout, plan: Plan, dq=None, dk=None, dv=None, workspace=None,
                         scale=None, stream=None):
-    _chk(q, k, v, out, lse, dout)
+    """dq, dk, dv bf16 and `workspace` (libra_attn_pool_bwd_workspace_bytes of this plan: plans of the same size may differ) are
+    allocated with torch when not given."""
     dq = torch.empty_like(q) if dq is None else dq
     dk = torch.empty_like(k) if dk is None else dk
     dv = torch.empty_like(v) if dv is None else dv
-    if workspace is None:
-        workspace = torch.empty(libra_attn_pool_bwd_workspace_bytes(plan, q, k), dtype=torch.uint8, device=q.device)
+    _chk_bwd(q, k, v, out, lse, dout, dq, dk, dv)
+    workspace = _workspace(workspace, libra_attn_pool_bwd_workspace_bytes(plan, q, k), q)
     dims = _dims(q, k, plan, scale)
     _check(_lib.libra_attn_pool_bwd(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), _ptr(dout),
                                     _ptr(plan.cu_seqlens), plan._h, _ptr(dq), _ptr(dk), _ptr(dv), _ptr(workspace),
@@ -263,7 +296,7 @@ def libra_attn_pool_bwd_noalloc_max_bytes() -> int:
 def libra_attn_pool_bwd_noalloc(q, k, v, out, lse, dout, plan: Plan, dq, dk, dv, scale=None, stream=None):
     """Backward that takes no workspace and allocates nothing: dq, dk, dv must be passed in.
     Raises LibraError(ERR_SCRATCH_TOO_SMALL) when the pool exceeds the library's built-in scratch."""
-    _chk(q, k, v, out, lse, dout, dq, dk, dv)
+    _chk_bwd(q, k, v, out, lse, dout, dq, dk, dv)
     dims = _dims(q, k, plan, scale)
     _check(_lib.libra_attn_pool_bwd_noalloc(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), _ptr(dout),
                                             _ptr(plan.cu_seqlens), plan._h, _ptr(dq), _ptr(dk), _ptr(dv),
@@ -370,16 +403,16 @@ def libra_attn_pool_bwd_ckpt8_workspace_bytes(plan: Plan, ckpt: Ckpt8) -> int:
 
 def libra_attn_pool_bwd_ckpt8(ckpt: Ckpt8, lse, dout, plan: Plan, dq=None, dk=None, dv=None, workspace=None, scale=None,
                               stream=None):
-    """Backward of the tensors that `ckpt` stands for -> dq, dk, dv."""
+    """Backward of the tensors that `ckpt` stands for -> dq, dk, dv.  `workspace`: libra_attn_pool_bwd_ckpt8_workspace_bytes of this
+    plan, which is more than libra_attn_pool_bwd takes (the restored q, k and v)."""
     c, dims = _ckpt8_dims(ckpt, plan, scale)
-    _chk(lse, dout)
-    assert dout.dtype == torch.bfloat16 and dout.shape == ckpt.q.shape
-    assert lse.dtype == torch.float32 and lse.shape == (dims.hq, dims.total_tokens)
+    assert dout.shape == ckpt.q.shape and lse.shape == (dims.hq, dims.total_tokens)
     new = lambda like: torch.empty(like.shape, dtype=torch.bfloat16, device=like.device)  # noqa: E731
     dq, dk, dv = new(ckpt.q) if dq is None else dq, new(ckpt.k) if dk is None else dk, new(ckpt.v) if dv is None else dv
-    _chk(dq, dk, dv)
-    if workspace is None:
-        workspace = torch.empty(libra_attn_pool_bwd_ckpt8_workspace_bytes(plan, ckpt), dtype=torch.uint8, device=dout.device)
+    _given("lse", lse, lse.numel(), torch.float32, ckpt.q)
+    for what, t, like in (("dout", dout, ckpt.q), ("dq", dq, ckpt.q), ("dk", dk, ckpt.k), ("dv", dv, ckpt.v)):
+        _given(what, t, like.numel(), torch.bfloat16, ckpt.q)
+    workspace = _workspace(workspace, int(_lib.libra_attn_pool_bwd_ckpt8_workspace_bytes(plan._h, ctypes.byref(dims))), dout)
     _check(_lib.libra_attn_pool_bwd_ckpt8(ctypes.byref(c), _ptr(lse), _ptr(dout), _ptr(plan.cu_seqlens), plan._h, _ptr(dq),
                                           _ptr(dk), _ptr(dv), _ptr(workspace), ctypes.byref(dims), _stream(stream)),
            "libra_attn_pool_bwd_ckpt8")
