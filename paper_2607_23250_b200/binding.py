@@ -9,6 +9,8 @@ from __future__ import annotations
 
 import collections
 import ctypes
+import functools
+import inspect
 import os
 
 import numpy as np
@@ -84,6 +86,23 @@ def _np(a):
 def _stream(stream=None):
     s = torch.cuda.current_stream() if stream is None else stream
     return _vp(s.cuda_stream)
+
+
+def _on_its_stream(f):
+    """f(..., stream=s) as `with torch.cuda.stream(s): f(...)`: tensors and workspaces that the call allocates belong to s.  (Of the
+    current stream's memory, one that is freed at the end of the call would be handed out again while the kernels on s still use it.)"""
+    at = list(inspect.signature(f).parameters).index("stream")
+
+    @functools.wraps(f)
+    def call(*args, **kw):
+        stream = args[at] if len(args) > at else kw.get("stream")
+        if stream is None:
+            return f(*args, **kw)
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(stream.cuda_stream)
+        with torch.cuda.stream(stream):
+            return f(*args, **kw)
+    return call
 
 
 def libra_selftest_wait_timeout(limit_ns: int):
@@ -255,6 +274,7 @@ def _chk_bwd(q, k, v, out, lse, dout, dq, dk, dv):
         _given(what, t, size, torch.bfloat16, q)
 
 
+@_on_its_stream
 def libra_attn_pool_fwd(q, k, v, plan: Plan, out=None, lse=None, scale=None, stream=None):
     """out [T,Hq,d] bf16, lse [Hq,T] fp32 (allocated with torch when not given)."""
     T, hq, _ = _chk_qkv(q, k, v)
@@ -273,6 +293,7 @@ def libra_attn_pool_bwd_workspace_bytes(plan: Plan, q, k) -> int:
     return int(_lib.libra_attn_pool_bwd_workspace_bytes(plan._h, ctypes.byref(dims)))
 
 
+@_on_its_stream
 def libra_attn_pool_bwd(q, k, v, out, lse, dout, plan: Plan, dq=None, dk=None, dv=None, workspace=None,
                         scale=None, stream=None):
     """dq, dk, dv bf16 and `workspace` (libra_attn_pool_bwd_workspace_bytes of this plan: plans of the same size may differ) are
@@ -352,6 +373,7 @@ def _packed(shapes, dtype, device):
     return out
 
 
+@_on_its_stream
 def libra_ckpt8_pack(q=None, k=None, v=None, out=None, ckpt: Ckpt8 = None, stream=None) -> Ckpt8:
     """8-bit checkpoint of the bf16 tensors given (q, out [T, Hq, d], k, v [T, Hkv, d]); into `ckpt` when that is given, else
     into memory of its own, all of it one allocation."""
@@ -373,6 +395,7 @@ def libra_ckpt8_pack(q=None, k=None, v=None, out=None, ckpt: Ckpt8 = None, strea
     return ckpt
 
 
+@_on_its_stream
 def libra_ckpt8_unpack(ckpt: Ckpt8, q=None, k=None, v=None, out=None, stream=None):
     """(q, k, v, out) as bf16, into the tensors given, None for those that the checkpoint does not hold."""
     c, dims = _ckpt8_args(ckpt)
@@ -401,6 +424,7 @@ def libra_attn_pool_bwd_ckpt8_workspace_bytes(plan: Plan, ckpt: Ckpt8) -> int:
     return int(_lib.libra_attn_pool_bwd_ckpt8_workspace_bytes(plan._h, ctypes.byref(_ckpt8_dims(ckpt, plan, None)[1])))
 
 
+@_on_its_stream
 def libra_attn_pool_bwd_ckpt8(ckpt: Ckpt8, lse, dout, plan: Plan, dq=None, dk=None, dv=None, workspace=None, scale=None,
                               stream=None):
     """Backward of the tensors that `ckpt` stands for -> dq, dk, dv.  `workspace`: libra_attn_pool_bwd_ckpt8_workspace_bytes of this
@@ -419,6 +443,7 @@ def libra_attn_pool_bwd_ckpt8(ckpt: Ckpt8, lse, dout, plan: Plan, dq=None, dk=No
     return dq, dk, dv
 
 
+@_on_its_stream
 def libra_vrsp_work(sample_offsets: torch.Tensor, seq_first_sample: torch.Tensor, stream=None) -> torch.Tensor:
     """F_i = sum of squared raw-sample lengths of packed sequence i (int64, on the device)."""
     for t in (sample_offsets, seq_first_sample):
@@ -430,6 +455,7 @@ def libra_vrsp_work(sample_offsets: torch.Tensor, seq_first_sample: torch.Tensor
     return work
 
 
+@_on_its_stream
 def libra_vrsp_place(work: torch.Tensor, pool_size: int, stream=None):
     """Algorithm 1 on the device -> dict(order, pool_of_seq, pool_load) of device tensors."""
     assert work.is_cuda and work.dtype == torch.int64 and work.is_contiguous()
@@ -452,6 +478,7 @@ class TapOpts(ctypes.Structure):
 _lib.libra_tap_num_tiles.restype = ctypes.c_int64
 
 
+@_on_its_stream
 def libra_tap_plan(cu_seqlens: torch.Tensor, seq_offsets, cp: int, block: int, n_shards: int, hq: int, hkv: int,
                    head_dim: int, tau_num: int = 3, tau_den: int = 100, stream=None):
     """Tiles, Algorithm 2 and the exchange volumes of one pool -> dict of device tensors
@@ -476,6 +503,7 @@ def libra_tap_plan(cu_seqlens: torch.Tensor, seq_offsets, cp: int, block: int, n
     return out
 
 
+@_on_its_stream
 def libra_tap_schedule(cu_seqlens: torch.Tensor, seq_offsets, sigma: torch.Tensor, cp: int, block: int, n_shards: int,
                        hq: int, hkv: int, head_dim: int, capacity: int = 0, stream=None) -> torch.Tensor:
     """Transfer records [n, 6] (kind, src, dst, tok0, ntok, shard) implied by assignment `sigma` (device int32).

@@ -101,3 +101,44 @@ def test_tensors_of_another_size_type_or_place(calls, name, tensors):
             with pytest.raises(AssertionError):
                 _call(name, {**a, t: bad})
     assert not any(c in ENTRY.values() for c in calls.made)
+
+
+@pytest.mark.parametrize("name", ["fwd", "bwd", "ckpt8", "pack", "unpack", "vrsp_work", "vrsp_place"])
+def test_what_a_call_on_another_stream_allocates_belongs_to_it(calls, monkeypatch, name):
+    """Memory of the current stream that is freed when the call returns would be another tensor's while the kernels still run."""
+    now, allocated = [None], []
+
+    class On:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            now.append(self.stream)
+
+        def __exit__(self, *_):
+            now.pop()
+
+    def recorded(f):
+        def call(*args, **kw):
+            allocated.append(now[-1])
+            return f(*args, **kw).as_subclass(Dev)
+        return call
+
+    a = _args()
+    work, offsets = _t(4, dtype=torch.int64), _t(5, dtype=torch.int32)
+    run = {"fwd": lambda **kw: lb.libra_attn_pool_fwd(a["q"], a["k"], a["v"], PLAN, **kw),
+           "bwd": lambda **kw: lb.libra_attn_pool_bwd(a["q"], a["k"], a["v"], a["out"], a["lse"], a["dout"], PLAN, **kw),
+           "ckpt8": lambda **kw: lb.libra_attn_pool_bwd_ckpt8(a["ckpt"], a["lse"], a["dout"], PLAN, **kw),
+           "pack": lambda **kw: lb.libra_ckpt8_pack(a["q"], a["k"], a["v"], a["out"], **kw),
+           "unpack": lambda **kw: lb.libra_ckpt8_unpack(a["ckpt"], **kw),
+           "vrsp_work": lambda **kw: lb.libra_vrsp_work(offsets, offsets, **kw),
+           "vrsp_place": lambda **kw: lb.libra_vrsp_place(work, 2, **kw)}[name]
+    monkeypatch.setattr(torch, "empty", recorded(torch.empty))
+    monkeypatch.setattr(torch, "empty_like", recorded(torch.empty_like))
+    monkeypatch.setattr(torch.cuda, "stream", On)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda p: ("stream", p))
+    run(stream=SimpleNamespace(cuda_stream=77))
+    assert allocated and all(s == ("stream", 77) for s in allocated)
+    allocated.clear()
+    run()
+    assert allocated and all(s is None for s in allocated) and now == [None]

@@ -200,6 +200,30 @@ def test_a_training_layer_captured_on_a_stream():
     plan.destroy()
 
 
+def test_calls_on_another_stream_keep_their_memory():
+    """Checkpoint, its reading and the backward pass on a stream that is behind: what they allocated is not handed to tensors of the
+    current stream when they return."""
+    from paper_2607_23250_b200 import binding as lb
+    cu, plan, xs, lse, dout = _layer(128, False, 130, 5)
+    want_ckpt = lb.libra_ckpt8_pack(*xs)
+    want_back = lb.libra_ckpt8_unpack(want_ckpt)
+    want = lb.libra_attn_pool_bwd_ckpt8(want_ckpt, lse, dout, plan)
+    size = lb.libra_attn_pool_bwd_ckpt8_workspace_bytes(plan, want_ckpt)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)                          # some 10 ms
+    ckpt = lb.libra_ckpt8_pack(*xs, stream=side)
+    back = lb.libra_ckpt8_unpack(ckpt, stream=side)
+    grads = lb.libra_attn_pool_bwd_ckpt8(ckpt, lse, dout, plan, stream=side)
+    others = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in (size, size // 2, 2 * size) for _ in range(2)]
+    torch.cuda.synchronize()
+    for got, exp in ((ckpt, want_ckpt), (back, want_back), (grads, want)):
+        assert all(torch.equal(x, y) for x, y in zip(got, exp))
+    assert all(bool((o == 255).all()) for o in others)
+    plan.destroy()
+
+
 def test_kernel_times_and_launch_counts():
     from paper_2607_23250_b200 import binding as lb
     cu, plan, xs, lse, dout = _layer(128, True, 60, 2)
