@@ -693,8 +693,9 @@ constexpr int kPrepRows = 8 * 256 / D;
 // Readers and clearers: of the first `spread` CTAs every period-th is of the rarer kind.
 struct PrepMix { uint32_t period, spread, clear_is_rare; };
 constexpr int64_t kPrepManyWarps = 24576;
-// HELD: out from a checkpoint, its integers and exponents.  A lane's eight values lie in one run, so its sum is scaled once;
-// by a power of two, so that it is bit for bit the sum over the values read back.  The CTAs that clear also restore q, k and v:
+// HELD: out from a checkpoint, its integers and exponents.  The integers are scaled ahead of the products, which is exact, so that the sum is
+// bit for bit that over the values read back.  (A sum over integers, scaled once, would be so only inside fp32's range: 127 times a
+// gradient above 2^121 is beyond it, however small the run's values are.)  The CTAs that clear also restore q, k and v:
 // those behind the first n_clear_ctas of them.
 struct RestoreArgs {
     CkptTensor t[3];
@@ -756,6 +757,7 @@ __global__ void k_bwd_prep(const void* __restrict__ out_, const uint8_t* __restr
 #pragma unroll
             for (int u = 0; u < STEPSH; ++u) {
                 const uint32_t* x = reinterpret_cast<const uint32_t*>(&a[u]);
+                const float up = run_up(e[u]);
                 float acc[2];
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
@@ -763,13 +765,14 @@ __global__ void k_bwd_prep(const void* __restrict__ out_, const uint8_t* __restr
                     float held[8];
                     held_floats(x[2 * k], held);
                     held_floats(x[2 * k + 1], held + 4);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) held[i] *= up;
                     acc[k] = 0.f;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float2 fb = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&y[i]));
                         acc[k] += held[2 * i] * fb.x + held[2 * i + 1] * fb.y;
                     }
-                    acc[k] *= run_up(e[u]);
 #pragma unroll
                     for (int off = LPRH / 2; off > 0; off >>= 1) acc[k] += __shfl_xor_sync(0xffffffffu, acc[k], off);
                 }

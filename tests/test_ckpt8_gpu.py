@@ -127,6 +127,26 @@ def test_backward_out_of_a_checkpoint(d, fused, window, sinks):
     plan.destroy()
 
 
+@pytest.mark.parametrize("d,fused", [(64, False), (128, False), (128, True), (256, False)])
+def test_row_statistics_at_the_ends_of_the_range(d, fused):
+    """Gradients near fp32's largest numbers against values of 2^-110, and the other way round: the products are ordinary
+    numbers, 127 times such a gradient is not.  Powers of two change no rounding, so dq and dk only scale."""
+    from paper_2607_23250_b200 import binding as lb
+    cu, plan, (q, k, v, out), lse, dout = _layer(d, fused, 40, 3, seed=d)
+    dout = dout.clamp(-3, 3)
+    base = lb.libra_attn_pool_bwd_ckpt8(lb.libra_ckpt8_pack(q, k, v, out), lse, dout, plan)
+    for down, up in ((110, 121), (-100, -100)):
+        v2, out2, dout2 = v * 2.0 ** -down, out * 2.0 ** -down, dout * 2.0 ** up
+        ckpt = lb.libra_ckpt8_pack(q, k, v2, out2)
+        grads = lb.libra_attn_pool_bwd_ckpt8(ckpt, lse, dout2, plan)
+        again = lb.libra_attn_pool_bwd(*lb.libra_ckpt8_unpack(ckpt), lse, dout2, plan)
+        assert all(bool(torch.isfinite(x).all()) for x in grads)
+        if not fused:
+            assert all(torch.equal(x, y) for x, y in zip(grads, again))
+            assert all(torch.equal(x, y * 2.0 ** (up - down)) for x, y in zip(grads[:2], base[:2]))
+    plan.destroy()
+
+
 def test_backward_on_pairs_of_ctas_and_over_dout():
     """The fused form on pairs of CTAs; dq written over dout."""
     from paper_2607_23250_b200 import binding as lb
