@@ -38,6 +38,35 @@ def test_half_a_step():
     assert np.array_equal(ref.value(q2, e2), ref.value(q, e))
 
 
+def test_gradients_of_the_layer_on_the_values_read_back():
+    """With lse and out of the values read back, dv is the gradient of that forward pass, and dq and dk are as far from it as
+    the rounding of out moves the row sums <dout, out>: half a step of each value.  With lse of the values before, rows of P do not
+    add up to 1."""
+    import window_reference as wref
+    T, h, d, window, sinks = 300, 2, 64, 120, 4
+    g = torch.Generator().manual_seed(5)
+    q, k, v, dout = (torch.randn((T, h, d), generator=g).to(torch.bfloat16) for _ in range(4))
+    see = wref.visible([0, T], window, sinks)
+    def held(x):
+        return torch.from_numpy(ref.value(*ref.held(x)))
+    Q, K, V = held(6 * q), held(k), held(v)
+    out, lse, *_ = wref.forward(Q, K, V, see)
+    given = out.to(torch.bfloat16)
+    exact, _ = wref.backward(Q, K, V, out, lse, dout, see)
+    got, _ = wref.backward(Q, K, V, held(given), lse, dout, see)
+    e = ref.held(given)[1].astype(int)
+    step = torch.from_numpy(np.ldexp(0.5, e - 133)).repeat_interleave(32, -1) + out.abs() * 2.0 ** -8     # and out's to bf16
+    off = (step * dout.abs().double()).sum(-1).t().unsqueeze(-1)                                          # of <dout, out> [h, T, 1]
+    p = torch.exp((Q.transpose(0, 1) @ K.transpose(0, 1).transpose(1, 2)) * d ** -0.5 - lse.unsqueeze(-1)).masked_fill(~see, 0)
+    assert torch.allclose(p.sum(-1), torch.ones(h, T, dtype=torch.float64), rtol=0, atol=1e-12)
+    bound_q = ((p * off) @ K.abs().transpose(0, 1)).transpose(0, 1) * d ** -0.5
+    bound_k = ((p * off).transpose(1, 2) @ Q.abs().transpose(0, 1)).transpose(0, 1) * d ** -0.5
+    assert torch.equal(got[2], exact[2])
+    assert bool(((got[0] - exact[0]).abs() <= bound_q + 1e-12).all()) and bool(((got[1] - exact[1]).abs() <= bound_k + 1e-12).all())
+    _, lse_before, *_ = wref.forward((6 * q), k, v, see)
+    assert float((torch.exp(lse - lse_before) - 1).abs().max()) > 0.05
+
+
 class Dims(ctypes.Structure):
     _fields_ = [("total_tokens", ctypes.c_int64), ("n_samples", ctypes.c_int), ("hq", ctypes.c_int), ("hkv", ctypes.c_int),
                 ("head_dim", ctypes.c_int), ("softmax_scale", ctypes.c_float)]

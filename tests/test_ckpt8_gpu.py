@@ -127,6 +127,35 @@ def test_backward_out_of_a_checkpoint(d, fused, window, sinks):
     plan.destroy()
 
 
+@pytest.mark.parametrize("d,fused", [(64, False), (128, False), (128, True), (256, False), (256, True)])
+def test_forward_on_the_values_read_back(d, fused):
+    """q, k and v packed ahead of a forward pass on what is read back, with scores that are large: against 64 bits, and rows of P
+    that add up to 1, so that dv of a sample adds up to its dout.  P and dv are rounded to bf16, half a step each, and lse
+    and the scores are off by the bound of lse each."""
+    from paper_2607_23250_b200 import binding as lb
+    cu, plan, (q, k, v, _), _, dout = _layer(d, fused, 130, 5, seed=d)
+    ckpt = lb.libra_ckpt8_pack(6 * q, k, v, torch.zeros_like(q))
+    q2, k2, v2, _ = lb.libra_ckpt8_unpack(ckpt)
+    out, lse = lb.libra_attn_pool_fwd(q2, k2, v2, plan)
+    lb.libra_ckpt8_pack(out=out, ckpt=ckpt)
+    grads = lb.libra_attn_pool_bwd_ckpt8(ckpt, lse, dout, plan)
+    vals = [torch.from_numpy(ref.value(x.cpu().numpy(), e.cpu().numpy())).cuda() for x, e in zip(ckpt[:4], ckpt[4:])]
+    assert all(torch.equal(x.double(), y) for x, y in zip((q2, k2, v2), vals))
+    see = wref.visible(cu, 130, 5, "cuda")
+    want, bounds = wref.backward(*vals, lse, dout, see)
+    for name, x, w, b in zip(("dq", "dk", "dv"), grads, want, bounds):
+        assert wref.worst(x, w, b) <= 1, name
+    *_, b_lse = wref.forward(*vals[:3], see)
+    heads = q.shape[1] // k.shape[1]
+    for a, z in zip(cu[:-1], cu[1:]):
+        g = dout[a:z].double()
+        total = g.sum(0).view(-1, heads, d).sum(1)
+        rows = (g.abs() * (1.01 * wref.U + 2.0 ** -18 + 2 * b_lse[:, a:z].t().unsqueeze(-1))).sum(0).view(-1, heads, d).sum(1)
+        room = 1.01 * rows + wref.U * 1.02 * grads[2][a:z].double().abs().sum(0) + 1e-30
+        assert bool(((grads[2][a:z].double().sum(0) - total).abs() <= room).all())
+    plan.destroy()
+
+
 @pytest.mark.parametrize("d,fused", [(64, False), (128, False), (128, True), (256, False)])
 def test_row_statistics_at_the_ends_of_the_range(d, fused):
     """Gradients near fp32's largest numbers against values of 2^-110, and the other way round: the products are ordinary
