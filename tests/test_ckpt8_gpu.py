@@ -176,6 +176,65 @@ def test_row_statistics_at_the_ends_of_the_range(d, fused):
     plan.destroy()
 
 
+@pytest.mark.parametrize("sinks", [0, 5, 200])
+def test_backward_where_the_library_chose_the_two_kernel_form(sinks):
+    """Pair tiles asked for, two kernels taken: statistics, partial sums of sinks' tails and the restored tensors share a workspace
+    of exactly the size that is asked for."""
+    from paper_2607_23250_b200 import binding as lb
+    cu, plan, xs, lse, dout = _layer(128, True, 130, sinks, n_workers=12)
+    assert plan.fused_ctas() == 0
+    ckpt = lb.libra_ckpt8_pack(*xs)
+    size = lb.libra_attn_pool_bwd_ckpt8_workspace_bytes(plan, ckpt)
+    room = torch.full((size + 4096,), 171, dtype=torch.uint8, device="cuda")
+    grads = lb.libra_attn_pool_bwd_ckpt8(ckpt, lse, dout, plan, workspace=room[:size])
+    again = lb.libra_attn_pool_bwd(*lb.libra_ckpt8_unpack(ckpt), lse, dout, plan)
+    torch.cuda.synchronize()
+    plan.busy_times(lb.KERNEL_BWD_DQ)
+    assert all(torch.equal(x, y) for x, y in zip(grads, again))
+    assert bool((room[size:] == 171).all())
+    vals = [torch.from_numpy(ref.value(q.cpu().numpy(), e.cpu().numpy())).cuda() for q, e in zip(ckpt[:4], ckpt[4:])]
+    want, bounds = wref.backward(*vals, lse, dout, wref.visible(cu, 130, sinks, "cuda"))
+    for name, g, w, b in zip(("dq", "dk", "dv"), grads, want, bounds):
+        assert wref.worst(g, w, b) <= 1, name
+    with pytest.raises(AssertionError):
+        lb.libra_attn_pool_bwd_ckpt8(ckpt, lse, dout, plan, workspace=room[:size - 1])
+    plan.destroy()
+
+
+def test_tensors_of_more_than_two_to_the_31_values():
+    """Offsets beyond 32 bits: the far end of a large tensor has the bits that it has by itself, and so have the gradients."""
+    from paper_2607_23250_b200 import binding as lb
+    T, hq, hkv, d = 70000, 256, 16, 128
+    cu = np.arange(0, T + 1, 1000, dtype=np.int32)
+    t = pools.make_tensors(T, hq, hkv, d, seed=1, device="cuda")
+    assert t["q"].numel() > 2 ** 31
+    plan = lb.libra_plan_tiles(torch.from_numpy(cu).cuda(), hq, 256, tile_kv=128, n_heads_kv=hkv, window=60, sinks=2)
+    out, lse = lb.libra_attn_pool_fwd(t["q"], t["k"], t["v"], plan)
+    xs = (t["q"], t["k"], t["v"], out)
+    ckpt = lb.libra_ckpt8_pack(*xs)
+    back = lb.libra_ckpt8_unpack(ckpt)
+    for part in (slice(0, 300), slice(T - 300, T)):
+        mine = lb.libra_ckpt8_pack(*(x[part] for x in xs))
+        assert all(torch.equal(a[part], b) for a, b in zip(ckpt, mine))
+        assert all(torch.equal(a[part], b) for a, b in zip(back, lb.libra_ckpt8_unpack(mine)))
+    grads = lb.libra_attn_pool_bwd_ckpt8(ckpt, lse, t["dout"], plan)
+    torch.cuda.synchronize()
+    plan.busy_times(lb.KERNEL_BWD_DQ)
+    again = lb.libra_attn_pool_bwd(*back, lse, t["dout"], plan)
+    assert all(torch.equal(x, y) for x, y in zip(grads, again))
+    a = T - 1000                                                # the last sample by itself, against 64 bits
+    see = wref.visible([0, 1000], 60, 2, "cuda")
+    G = hq // hkv
+    for h in (0, hkv - 1):
+        heads = slice(h * G, (h + 1) * G)
+        vals = [back[0][a:, heads].contiguous(), back[1][a:, h:h + 1].contiguous(), back[2][a:, h:h + 1].contiguous(), back[3][a:, heads].contiguous()]
+        want, bounds = wref.backward(*vals, lse[heads, a:], t["dout"][a:, heads], see)
+        got = grads[0][a:, heads], grads[1][a:, h:h + 1], grads[2][a:, h:h + 1]
+        for name, x, w, b in zip(("dq", "dk", "dv"), got, want, bounds):
+            assert wref.worst(x, w, b) <= 1, (name, h)
+    plan.destroy()
+
+
 def test_backward_on_pairs_of_ctas_and_over_dout():
     """The fused form on pairs of CTAs; dq written over dout."""
     from paper_2607_23250_b200 import binding as lb
@@ -189,6 +248,22 @@ def test_backward_on_pairs_of_ctas_and_over_dout():
         grads = lb.libra_attn_pool_bwd_ckpt8(ckpt, lse, g, plan, dq=g if over else None)
         for x, w, b in zip(grads, want, bounds):
             assert wref.worst(x, w, b) <= 1
+    plan.destroy()
+
+
+@pytest.mark.parametrize("window,sinks", [(3000, 0), (3500, 4), (4000, 200)])
+def test_windowed_backward_on_pairs_of_ctas(window, sinks):
+    from paper_2607_23250_b200 import binding as lb
+    cu, plan, xs, lse, dout = _layer(128, True, window, sinks, lengths=[100, 7400], hq=2, hkv=1, pair_chunk=512, n_workers=16)
+    assert plan.fused_ctas() == 2
+    ckpt = lb.libra_ckpt8_pack(*xs)
+    grads = lb.libra_attn_pool_bwd_ckpt8(ckpt, lse, dout, plan)
+    torch.cuda.synchronize()
+    plan.busy_times(lb.KERNEL_BWD_FUSED)
+    vals = [torch.from_numpy(ref.value(q.cpu().numpy(), e.cpu().numpy())).cuda() for q, e in zip(ckpt[:4], ckpt[4:])]
+    want, bounds = wref.backward(*vals, lse, dout, wref.visible(cu, window, sinks, "cuda"))
+    for name, g, w, b in zip(("dq", "dk", "dv"), grads, want, bounds):
+        assert wref.worst(g, w, b) <= 1, name
     plan.destroy()
 
 

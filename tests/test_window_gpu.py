@@ -193,6 +193,85 @@ def test_the_longest_pool_of_the_two_kernel_form(window, sinks):
     plan.destroy()
 
 
+@pytest.mark.parametrize("lengths,window,sinks", [([700, 40, 500], 120, 4), ([9000, 300], 500, 0), ([200, 5000], 900, 140)])
+@pytest.mark.parametrize("hq,hkv,shards", [(4, 2, 2), (4, 1, 1), (6, 2, 2)])
+@pytest.mark.parametrize("d,fused", FORMS)
+def test_several_heads_a_shard(d, fused, hq, hkv, shards, lengths, window, sinks):
+    """Query-major tiles of more than one head: few tiles, with a CTA for each half, and many."""
+    from paper_2607_23250_b200 import binding as lb
+    cu = pools.cu_seqlens(lengths)
+    q, k, v, dout = _tensors(cu, hq, hkv, d, window)
+    directions = lb.LIBRA_DIR_Q | (lb.LIBRA_DIR_PAIR if fused else lb.LIBRA_DIR_KV)
+    plan = lb.libra_plan_tiles(torch.from_numpy(cu).cuda(), shards, 256, directions=directions, tile_kv=128, n_heads_kv=hkv,
+                               window=window, sinks=sinks)
+    assert plan.status() == 0
+    _check(cu, q, k, v, dout, _run(plan, q, k, v, dout, fused), window, sinks)
+    plan.destroy()
+
+
+@pytest.mark.parametrize("scale", [0.03, 0.4])
+@pytest.mark.parametrize("d,fused", FORMS)
+def test_a_scale_that_is_given(d, fused, scale):
+    from paper_2607_23250_b200 import binding as lb
+    cu = pools.cu_seqlens([600, 150])
+    q, k, v, dout = _tensors(cu, 4, 2, d, 12)
+    plan = _plan(cu, 4, 2, fused, 110, 3)
+    out, lse = lb.libra_attn_pool_fwd(q, k, v, plan, scale=scale)
+    grads = lb.libra_attn_pool_bwd(q, k, v, out, lse, dout, plan, scale=scale)
+    see = ref.visible(cu, 110, 3, "cuda")
+    o, l, b_o, b_l = ref.forward(q, k, v, see, scale)
+    assert ref.worst(out, o, b_o) <= 1 and ref.worst(lse, l, b_l) <= 1
+    want, bounds = ref.backward(q, k, v, out, lse, dout, see, scale)
+    for name, g, w, b in zip(("dq", "dk", "dv"), grads, want, bounds):
+        assert ref.worst(g, w, b) <= 1, name
+    plan.destroy()
+
+
+@pytest.mark.parametrize("over", ["q", "dout"])
+@pytest.mark.parametrize("workers", [0, 12])
+@pytest.mark.parametrize("d,fused", FORMS)
+def test_dq_in_place(d, fused, workers, over):
+    """dq written over q or dout: with CTAs for every tile and with few; a fused plan of few workers takes the two-kernel form."""
+    from paper_2607_23250_b200 import binding as lb
+    cu = pools.cu_seqlens([900, 300])
+    q, k, v, dout = _tensors(cu, 4, 2, d, 2)
+    plan = _plan(cu, 4, 2, fused, 150, 3, n_workers=workers)
+    out, lse = lb.libra_attn_pool_fwd(q, k, v, plan)
+    x = {"q": q.clone(), "dout": dout.clone()}
+    grads = lb.libra_attn_pool_bwd(x["q"], k, v, out, lse, x["dout"], plan, dq=x[over])
+    assert grads[0] is x[over]
+    _check(cu, q, k, v, dout, (out, lse, grads), 150, 3)
+    plan.destroy()
+
+
+@pytest.mark.parametrize("sinks", [0, 4])
+@pytest.mark.parametrize("d", [64, 256])
+def test_a_plan_built_under_capture(d, sinks):
+    """The plan holds what the last replay computed, the tails of sinks too."""
+    from paper_2607_23250_b200 import binding as lb
+    layouts = [pools.cu_seqlens(x) for x in ([700, 500, 1], [1, 1150, 50])]
+    q, k, v, dout = _tensors(layouts[0], 2, 1, d, 7)
+    cu = torch.from_numpy(layouts[0]).cuda()
+    _plan(layouts[0], 2, 1, False, 200, sinks).destroy()            # what a first call sets up is there
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side, capture_error_mode="relaxed"):
+        plan = lb.libra_plan_tiles(cu, 2, 256, tile_kv=128, n_heads_kv=1, total_tokens=1201, window=200, sinks=sinks)
+    for layout in layouts:
+        cu.copy_(torch.from_numpy(layout))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert plan.status() == 0
+        _check(layout, q, k, v, dout, _run(plan, q, k, v, dout, False), 200, sinks)
+    del graph
+    plan.destroy()
+
+
+@pytest.mark.parametrize("d,fused,window,sinks", [(64, False, 1000, 4), (128, False, 300, 0), (128, True, 5000, 130), (256, False, 2000, 2)])
+def test_a_pool_of_twelve_thousand_tokens(d, fused, window, sinks):
+    _case([700, 10100, 1200], 2, 1, d, fused, window, sinks, seed=d)
+
+
 @pytest.mark.parametrize("d,fused", FORMS)
 def test_a_window_that_reaches_everything_changes_nothing(d, fused):
     from paper_2607_23250_b200 import binding as lb
