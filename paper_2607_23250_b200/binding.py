@@ -161,8 +161,13 @@ class Plan:
         return n
 
     def busy_times(self, which=KERNEL_FWD):
-        w = self.info(LIBRA_DIR_PAIR if which == KERNEL_BWD_FUSED else
-                      (LIBRA_DIR_KV if which == KERNEL_BWD_DKDV else LIBRA_DIR_Q))["n_workers"]
+        direction = LIBRA_DIR_PAIR if which == KERNEL_BWD_FUSED else (LIBRA_DIR_KV if which == KERNEL_BWD_DKDV else LIBRA_DIR_Q)
+        try:
+            w = self.info(direction)["n_workers"]
+        except LibraError:
+            if which != KERNEL_BWD_DKDV:
+                raise
+            w = self.info(LIBRA_DIR_Q)["n_workers"]   # key-major lists may be the library's own; all directions have as many
         out = np.zeros(w, np.uint64)
         _check(_lib.libra_busy_times(self._h, which, _np(out)), "libra_busy_times")
         return out

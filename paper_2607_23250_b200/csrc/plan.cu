@@ -1152,6 +1152,7 @@ extern "C" int libra_busy_times(const libra_plan_t* plan, int which, uint64_t* n
     // backward the pair tiles
     PlanDir* d = any_dir(plan, which == LIBRA_KERNEL_BWD_FUSED ? LIBRA_DIR_PAIR
                                                                : (which == LIBRA_KERNEL_BWD_DKDV ? LIBRA_DIR_KV : LIBRA_DIR_Q));
+    if (which == LIBRA_KERNEL_BWD_DKDV && !(plan->asked & LIBRA_DIR_KV) && !plan->two_kernel) d = nullptr;   // no kernel walks such lists
     if (!d) return LIBRA_ERR_PLAN_MISMATCH;
     if (cudaDeviceSynchronize() != cudaSuccess) return LIBRA_ERR_CUDA;
     const size_t most = (size_t)d->W + 1;

@@ -136,6 +136,29 @@ def test_the_form_of_the_backward():
 
 
 @pytest.mark.parametrize("sinks", [0, 3])
+def test_busy_times_of_the_form_that_was_chosen(sinks):
+    """Of the two kernels where the library took them for a plan with pair tiles, otherwise there is no dK/dV kernel to ask for."""
+    from paper_2607_23250_b200 import binding as lb
+    cu = pools.cu_seqlens([900, 300])
+    q, k, v, dout = _tensors(cu, 4, 2, 128, 2)
+    for workers in (12, 148):
+        plan = _plan(cu, 4, 2, True, 150, sinks, n_workers=workers)
+        out, lse = lb.libra_attn_pool_fwd(q, k, v, plan)
+        lb.libra_attn_pool_bwd(q, k, v, out, lse, dout, plan)
+        if workers == 12:
+            assert plan.fused_ctas() == 0
+            for kern in (lb.KERNEL_BWD_DKDV, lb.KERNEL_BWD_DQ):
+                busy = plan.busy_times(kern)
+                assert len(busy) == 12 and (busy > 0).all()
+        else:
+            assert plan.fused_ctas() == 1 and plan.busy_times(lb.KERNEL_BWD_FUSED).any()
+            with pytest.raises(lb.LibraError) as err:
+                plan.busy_times(lb.KERNEL_BWD_DKDV)
+            assert err.value.code == lb.ERR_PLAN_MISMATCH
+        plan.destroy()
+
+
+@pytest.mark.parametrize("sinks", [0, 3])
 @pytest.mark.parametrize("heads,tile", [(4, 128), (3, 256), (4, 384)])
 def test_plans_that_only_the_fused_form_can_take(heads, tile, sinks):
     """A pool for which the two-kernel form would be the faster one, but whose query-major lists its kernels cannot walk: tiles of
