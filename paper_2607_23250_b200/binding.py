@@ -225,7 +225,7 @@ def libra_plan_tiles(cu_seqlens: torch.Tensor, n_heads: int, tile_q: int, n_work
                     unit_cost_q, unit_cost_kv, pair_chunk)
     h = _vp()
     if window != 0 or sinks != 0:
-        window, sinks = min(window, 2 ** 31 - 1), min(sinks, 2 ** 31 - 1)   # (no sample is longer)
+        window, sinks = (max(-1, min(x, 2 ** 31 - 1)) for x in (window, sinks))   # (no sample is longer)
         _check(_lib.libra_plan_tiles_window(_ptr(cu_seqlens), ctypes.c_int(cu_seqlens.numel() - 1), ctypes.c_int(n_heads),
                                             ctypes.c_int(tile_q), ctypes.byref(opts), ctypes.c_int(window),
                                             ctypes.c_int(sinks), _stream(stream), ctypes.byref(h)),

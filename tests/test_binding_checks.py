@@ -142,3 +142,14 @@ def test_what_a_call_on_another_stream_allocates_belongs_to_it(calls, monkeypatc
     allocated.clear()
     run()
     assert allocated and all(s is None for s in allocated) and now == [None]
+
+
+@pytest.mark.parametrize("given,passed", [((5, 2), (5, 2)), ((2 ** 40, 2 ** 33), (2 ** 31 - 1, 2 ** 31 - 1)), ((-2 ** 32 + 5, 0), (-1, 0)),
+                                          ((7, -2 ** 32 + 3), (7, -1)), ((-2 ** 31 - 1, -2 ** 40), (-1, -1))])
+def test_windows_beyond_32_bits_do_not_wrap(monkeypatch, calls, given, passed):
+    """A window that is longer than any sample is none; one below zero stays what the library refuses."""
+    seen = []
+    monkeypatch.setattr(lb, "_lib", SimpleNamespace(libra_plan_tiles_window=lambda *a: seen.append((a[5].value, a[6].value)) or 0,
+                                                    libra_plan_destroy=lambda h: 0))
+    lb.libra_plan_tiles(_t(2, dtype=torch.int32), 1, 256, window=given[0], sinks=given[1])
+    assert seen == [passed]
