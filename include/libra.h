@@ -146,8 +146,9 @@ int libra_plan_tiles(const int32_t* cu_seqlens_dev, int n_samples, int n_heads, 
  * holds sinks are tiles of their own; their partial sums are added up in a fixed order, in its workspace.)
  * At head_dim 128 a plan with LIBRA_DIR_PAIR and LIBRA_DIR_Q leaves the backward's form to the library: the two-kernel form
  * (bit-reproducible, and without the fp32 accumulators in the workspace) where short windows make it the faster one and its
- * kernels can take the plan (tile_q == 256, at most 65536 key blocks, n_heads dividing hq in the call):
- * libra_plan_fused_ctas then returns 0 (whatever hq the call will have), and libra_busy_times and the kernel times are those of the dK/dV and dQ kernels.
+ * kernels can take the plan (tile_q == 256, at most 65536 key blocks, n_heads a multiple or a divisor of n_heads_kv; of
+ * such a plan n_heads must divide hq in the backward as in the forward, whichever form it takes).
+ * libra_plan_fused_ctas then returns 0, and libra_busy_times and the kernel times are those of the dK/dV and dQ kernels.
  * A window that is not below T gives what libra_plan_tiles gives, one that is not below any sample's length the same
  * results (with sinks up to rounding).  As there, an infinity or
  * a NaN of a key or value reaches rows that do not see it where they share a 128-row block with rows, and a key

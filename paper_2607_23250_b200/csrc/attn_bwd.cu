@@ -896,12 +896,8 @@ static BwdWorkspace bwd_workspace(int64_t T, int hq, int hkv, int d, bool fused,
 }
 // A plan with pair tiles selects the accumulating forms: at head_dim 128 the fused kernel (dQ, dK, dV accumulated in
 // fp32), at head_dim 256 the dV and dK passes over pair tiles (dK, dV accumulated in fp32; the dQ pass is unchanged).
-// The fused form does not walk the query-major lists: where their head shards do not divide the heads, it is the form that runs.
-static bool two_kernels_chosen(const libra_plan_t* plan, const libra_dims* dims) {
-    return plan->two_kernel && dims->hq % plan->dir[0].H == 0;
-}
 static bool use_fused(const libra_plan_t* plan, const libra_dims* dims) {
-    return plan->dir[2].enabled && ((dims->head_dim == 128 && !two_kernels_chosen(plan, dims)) || dims->head_dim == 256);
+    return plan->dir[2].enabled && ((dims->head_dim == 128 && !plan->two_kernel) || dims->head_dim == 256);
 }
 
 template <typename Kernel>
@@ -1010,7 +1006,8 @@ using namespace libra;
 
 // Tail tiles that a call cuts off the sinks' key blocks; none where it walks whole ones (tails false, or no such lists).
 static int tails_of(const libra_plan_t* plan, const libra_dims* dims, bool tails) {
-    return tails ? plan->dir[dims->head_dim == 256 ? 6 : 5].n_tails : 0;
+    const PlanDir& d = plan->dir[dims->head_dim == 256 ? 6 : 5];
+    return tails && d.enabled ? d.n_tails : 0;
 }
 
 namespace libra {
@@ -1039,7 +1036,6 @@ static int launch_fused(const void* q_dev, const void* k_dev, const void* v_dev,
     const int64_t T = plan->T;
     if (d.tile != kBlk || d.H != dims->hkv) return LIBRA_ERR_PLAN_MISMATCH;
     if (d.W > plan->sm_count) return LIBRA_ERR_UNSUPPORTED;
-    if (plan->two_kernel && list_pair_tiles(plan, s) != cudaSuccess) return LIBRA_ERR_CUDA;
     float* dvec = reinterpret_cast<float*>(ws_dev);
     float* lse2 = reinterpret_cast<float*>(ws_dev + ws.stat_bytes);
     float* dq_acc = reinterpret_cast<float*>(ws_dev + 2 * ws.stat_bytes);
@@ -1163,9 +1159,11 @@ static int backward(const void* q_dev, const void* k_dev, const void* v_dev, Row
         if (pd.tile != kBlk || pd.H != dims->hkv) return LIBRA_ERR_PLAN_MISMATCH;
         if (pd.W > plan->sm_count || dq_dir.W > plan->sm_count) return LIBRA_ERR_UNSUPPORTED;
     }
+    // which form a windowed plan takes is its pool's affair, what heads it takes is not
+    if (fused && dims->head_dim == 128 && plan->either_form && dims->hq % dq_dir.H) return LIBRA_ERR_INVALID_ARG;
     if (!fused) {
         if (!dq_dir.enabled || !dkv_dir.enabled) return LIBRA_ERR_PLAN_MISMATCH;
-        if (!(plan->asked & LIBRA_DIR_KV) && !(two_kernels_chosen(plan, dims) && dims->head_dim == 128)) return LIBRA_ERR_PLAN_MISMATCH;   // not the caller's lists
+        if (!(plan->asked & LIBRA_DIR_KV) && !(plan->two_kernel && dims->head_dim == 128)) return LIBRA_ERR_PLAN_MISMATCH;   // not the caller's lists
         if (dkv_dir.tile != kBlk || dq_dir.tile != 2 * kBlk) return LIBRA_ERR_UNSUPPORTED;
         if (dkv_dir.H != dims->hkv) return LIBRA_ERR_PLAN_MISMATCH;
         if (dims->hq % dq_dir.H) return LIBRA_ERR_INVALID_ARG;

@@ -70,6 +70,7 @@ struct libra_plan {
     int n_outcome[4] = {};           // CTAs of that launch: clusters leave the last workers out, pairs may add one
     int W = 0;                       // workers of every direction
     int asked = 0;                   // directions the caller asked for (key-major lists may be there for the library's own use)
+    int either_form = 0;             // a windowed plan with pair tiles that the two-kernel form at head_dim 128 could take as well
     int two_kernel = 0;              // pair tiles or not, the backward at head_dim 128 takes the two-kernel form (prefer_two_kernels)
     int bwd_mask = 0;                // which of d_outcome[1..3] the last backward wrote
     // 0 = query-major, 1 = key-major, 2 = pair tiles (key block x query chunk), 3 = the key-stationary tiles of kernels that
@@ -96,8 +97,6 @@ constexpr int kMaxDevices = 64;
 constexpr int kCfgSlots = 24;
 bool cfg_done(int slot);
 void cfg_mark(int slot);
-// Makes the lists of direction 2 where planning has left them out (two_kernel, or direction 4 there), the same ones at every call.
-cudaError_t list_pair_tiles(const libra_plan* plan, cudaStream_t s);
 // LIBRA_ERR_PLAN_MISMATCH when the current device is not the one the plan was built on.
 int check_plan_device(const libra_plan* plan);
 // Kernel timing (libra_plan_set_timing): events on the launch stream around kernel k (LIBRA_KERNEL_* - 1).

@@ -686,9 +686,8 @@ static bool fused_on_pairs(const libra_plan* p, int64_t cells, int64_t wide_cell
 // 802: 28 / 50 (33).  On pairs of CTAs: 65536 tokens, 32 / 4 heads, 4096: 11900 / 13800, 8192: 20900 / 24800.  On 160 pools of
 // 700 to 131072 tokens with windows of 32 to 8192 the choice is 1.2 % from the better form on average, always the fused
 // one 12 %, always the other 10 %.
-// The dQ kernel of that form takes query tiles of 256 rows; the fused one does not walk them, so plans with others keep it.
 static bool prefer_two_kernels(const libra_plan* p, bool on_pairs, int64_t cells) {
-    if (!p->window || on_pairs || p->dir[0].tile != 256) return false;
+    if (on_pairs) return false;
     return cells <= 8 * p->dir[1].NB && 100 * p->dir[1].NT >= (p->sinks ? 135 : 90) * p->W;
 }
 static double heads_per_kv(const libra_plan* p) { return p->dir[0].H > p->dir[2].H ? (double)p->dir[0].H / p->dir[2].H : 1.0; }
@@ -740,14 +739,6 @@ static void place_lists(const DirViews& views, int n, int max_w, int64_t max_nt,
     k_place<<<n, (max_w + 31) / 32 * 32, 0, s>>>(views);
     k_scatter_lists<<<dim3(grid_for(max_nt > 0 ? max_nt : 1, 256), n), 256, 0, s>>>(views);
     count_launch(2);
-}
-
-cudaError_t list_pair_tiles(const libra_plan* p, cudaStream_t s) {
-    const PlanDir& d = p->dir[2];
-    DirViews views = {};
-    views.v[0] = view_of(d, 1, libra_plan_opts{});
-    place_lists(views, 1, d.W, d.NT, s);
-    return cudaGetLastError();
 }
 
 // Builds the directions asked for; p->dir[k].tile / H / W / chunk are set.
@@ -875,9 +866,14 @@ static int build_plan(libra_plan* p, const int32_t* cu, const libra_plan_opts& o
         }
     }
     // ---- weights, order, placement and lists of all directions together
+    // The two-kernel form walks the query-major lists, 256 rows a tile and shards of whole heads.  The heads are not known here: shards
+    // that are a multiple or a divisor of the kv heads are taken to fit them (libra_attn_pool_bwd checks), others leave the fused form.
+    const int H = p->dir[0].H, Hkv = p->dir[2].H;
+    p->either_form = p->window && pairs[2] && sorted[0] && sorted[1] && (!p->sinks || sorted[5]) && p->dir[0].tile == 256 &&
+                     p->dir[1].tile == 128 && (H % Hkv == 0 || Hkv % H == 0);
+    p->two_kernel = p->either_form && prefer_two_kernels(p, pairs[4], cells);
     // Lists that no kernel walks are not made: the key-major ones of a windowed plan whose caller did not ask for them, unless the
     // two-kernel form was chosen and takes these; with it those of the pair tiles.
-    p->two_kernel = pairs[2] && sorted[0] && sorted[1] && (!p->sinks || sorted[5]) && prefer_two_kernels(p, pairs[4], cells);
     const bool live[kDirs] = {sorted[0], sorted[1] && (asked_kv || (p->two_kernel && !p->sinks)), false, sorted[3], false,
                               sorted[5] && (asked_kv || p->two_kernel), sorted[6]};
     DirViews views = {};
@@ -1076,8 +1072,12 @@ extern "C" int libra_plan_export(const libra_plan_t* plan, int direction, int64_
     if (weight_host || order_host) ok(cudaMalloc(&tmp, sizeof(int64_t) * (d->NT ? d->NT : 1)));
     if (e != cudaSuccess) return LIBRA_ERR_CUDA;
     // Pair tiles whose lists no kernel walks: made here, the same ones at every call.
-    if (d == &plan->dir[2] && (plan->dir[4].enabled || plan->two_kernel) && (cta_of_tile_host || cta_offsets_host || cta_tiles_host || loads_host))
-        ok(list_pair_tiles(plan, s));
+    if (d == &plan->dir[2] && (plan->dir[4].enabled || plan->two_kernel) && (cta_of_tile_host || cta_offsets_host || cta_tiles_host || loads_host)) {
+        DirViews views = {};
+        views.v[0] = view_of(*d, 1, libra_plan_opts{});
+        place_lists(views, 1, d->W, d->NT, s);
+        ok(cudaGetLastError());
+    }
     if (weight_host) {
         k_expand_weight<<<grid_for(d->NT, 256), 256, 0, s>>>(d->d_weight_blk, d->NT, d->H, d->d_u_blk ? d->NB : 0,
                                                              (int64_t*)tmp);

@@ -162,7 +162,7 @@ def test_busy_times_of_the_form_that_was_chosen(sinks):
 @pytest.mark.parametrize("heads,tile", [(4, 128), (3, 256), (4, 384)])
 def test_plans_that_only_the_fused_form_can_take(heads, tile, sinks):
     """A pool for which the two-kernel form would be the faster one, but whose query-major lists its kernels cannot walk: tiles of
-    another size, head shards that do not divide the heads.  The fused form needs neither."""
+    another size, head shards that fit the kv heads in no way.  The fused form needs neither."""
     from paper_2607_23250_b200 import binding as lb
     cu = pools.cu_seqlens([900, 300])
     q, k, v, dout = _tensors(cu, 4, 2, 128, 2)
@@ -171,7 +171,7 @@ def test_plans_that_only_the_fused_form_can_take(heads, tile, sinks):
     out, lse = lb.libra_attn_pool_fwd(q, k, v, first)
     plan = lb.libra_plan_tiles(torch.from_numpy(cu).cuda(), heads, tile, directions=lb.LIBRA_DIR_Q | lb.LIBRA_DIR_PAIR, tile_kv=128,
                                n_heads_kv=2, window=150, sinks=sinks, n_workers=12)
-    assert plan.status() == 0 and plan.fused_ctas() == (1 if tile != 256 else 0)
+    assert plan.status() == 0 and plan.fused_ctas() == 1
     assert (lb.libra_attn_pool_bwd_workspace_bytes(plan, q, k) > lb.libra_attn_pool_bwd_workspace_bytes(first, q, k))
     for _ in range(2):
         grads = lb.libra_attn_pool_bwd(q, k, v, out, lse, dout, plan)
@@ -180,6 +180,22 @@ def test_plans_that_only_the_fused_form_can_take(heads, tile, sinks):
         _check(cu, q, k, v, dout, (out, lse, grads), 150, sinks)
     first.destroy()
     plan.destroy()
+
+
+def test_head_shards_that_do_not_divide_the_heads():
+    """Refused by the plan of either form: the pool does not decide what is accepted."""
+    from paper_2607_23250_b200 import binding as lb
+    cu = pools.cu_seqlens([900, 300])
+    q, k, v, dout = _tensors(cu, 4, 2, 128, 2)
+    lse = torch.zeros((4, q.shape[0]), device="cuda")
+    for workers, ctas in ((12, 0), (148, 1)):
+        plan = _plan(cu, 8, 2, True, 150, 3, n_workers=workers)
+        assert plan.fused_ctas() == ctas
+        launches = lb.launch_count()
+        with pytest.raises(lb.LibraError) as err:
+            lb.libra_attn_pool_bwd(q, k, v, q, lse, dout, plan)
+        assert err.value.code == lb.ERR_INVALID_ARG and lb.launch_count() == launches
+        plan.destroy()
 
 
 @pytest.mark.parametrize("sinks", [0, 4])
