@@ -381,7 +381,7 @@ def _packed(shapes, dtype, device):
 @_on_its_stream
 def libra_ckpt8_pack(q=None, k=None, v=None, out=None, ckpt: Ckpt8 = None, stream=None) -> Ckpt8:
     """8-bit checkpoint of the bf16 tensors given (q, out [T, Hq, d], k, v [T, Hkv, d]); into `ckpt` when that is given, else
-    into memory of its own, all of it one allocation."""
+    into memory of its own, all of it one allocation: any of the tensors keeps all of it alive."""
     xs = (q, k, v, out)
     assert all(x is None or x.dtype is torch.bfloat16 for x in xs)
     dims = _ckpt8_dims_of(xs)
@@ -402,7 +402,9 @@ def libra_ckpt8_pack(q=None, k=None, v=None, out=None, ckpt: Ckpt8 = None, strea
 
 @_on_its_stream
 def libra_ckpt8_unpack(ckpt: Ckpt8, q=None, k=None, v=None, out=None, stream=None):
-    """(q, k, v, out) as bf16, into the tensors given, None for those that the checkpoint does not hold."""
+    """(q, k, v, out) as bf16, into the tensors given, None for those that the checkpoint does not hold.  Those not given are views of
+    one allocation: any of them keeps all alive, and they share a version counter, so that for autograd a change of one in place is
+    a change of all."""
     c, dims = _ckpt8_args(ckpt)
     xs = [q, k, v, out]
     for x, val in zip(xs, ckpt):

@@ -464,7 +464,9 @@ k_attn_bwd_dkdv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                      warp_wait(bar_dpfull, it_all & 1, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
-                uint32_t xs[64];   // (dP^T - D) as packed bf16 pairs
+                // (dP^T - D) as packed bf16 pairs: they wait for P^T, which comes as bf16 from the exp groups; in fp32 they
+                // would be 128 registers.  So dS carries three roundings of half a step, 2^-8: P's, theirs and the product's.
+                uint32_t xs[64];
                 {
                     uint32_t dpv[128];
                     tmem_ld128(t_x, dpv);

@@ -528,7 +528,9 @@ k_attn_bwd_pair(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 ok = watched_warp_wait(&bars[L::kDvecFull + (n & 1)], (n >> 1) & 1, abort_flag) && watched_warp_wait(&bars[L::kDpFull], n & 1, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
-                uint32_t xs[64];   // (dP^T - D) as packed bf16 pairs
+                // (dP^T - D) as packed bf16 pairs: they wait for P^T, which comes as bf16 from the exp groups; in fp32 they
+                // would be 128 registers.  So dS carries three roundings of half a step, 2^-8: P's, theirs and the product's.
+                uint32_t xs[64];
                 {
                     const uint64_t neg1 = f2_pack(-1.f, -1.f);
 #pragma unroll

@@ -7,6 +7,7 @@
 // above the run's largest magnitude.  (A bf16 below 2^E' x 2 is at most 255 / 128 x 2^E', so only 127.5 could round to
 // 128; clamped, it is half a step off as well.)  E = 255: the run holds an infinity or a NaN and reads as NaN.  With E >= 7
 // the factor 2^(133 - E) is a finite fp32 number; values below 2^-127 of such runs read as zero.
+// (The published MXINT8 layout, integers in blocks of 32 with a power of two each, with a floor on the exponent.)
 // An absolute scale per run (its largest magnitude / 127) would make the step up to two times finer, round what is read back once
 // more, to bf16, and take four bytes a run instead of one.
 #pragma once

@@ -406,7 +406,8 @@ def library_attention(device="cuda"):
     assembled from local and received rows) in the worker's own memory; the fragment is copied to the device, the
     query side is padded with zero rows in front so that it becomes one whole sample of a one-sample pool, and the
     library plans and runs it.  Zero query rows with zero upstream gradient contribute nothing to dK / dV, so the
-    padded call returns exactly the fragment's partial sums.  Planning a pool per fragment is the simple form: it
+    padded call returns exactly the fragment's partial sums.  The mask is that of a whole sample's past: layers with a window or
+    sinks are not split this way (by heads they are: sharding.py).  Planning a pool per fragment is the simple form: it
     serves to run the exchange with the real kernels; a production executor would batch a worker's fragments into
     one pool per chunk."""
     import torch
