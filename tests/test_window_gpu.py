@@ -433,6 +433,32 @@ def test_two_kernel_form_is_bit_reproducible_and_captured():
     plan.destroy()
 
 
+@pytest.mark.parametrize("d,fused", FORMS)
+def test_two_streams_share_a_plan(d, fused):
+    """A layer's passes on two streams at once, each with tensors and a workspace of its own."""
+    from paper_2607_23250_b200 import binding as lb
+    cu = pools.cu_seqlens([2600, 30, 1500])
+    plan = _plan(cu, 4, 2, fused, 300, 5)
+    ins = [_tensors(cu, 4, 2, d, seed) for seed in (1, 2)]
+    want = [_run(plan, *x, fused) for x in ins]
+    streams = [torch.cuda.Stream() for _ in ins]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(6):
+        for x, s, res in zip(ins, streams, got):
+            out, lse = lb.libra_attn_pool_fwd(*x[:3], plan, stream=s)
+            res.append((out, lse, lb.libra_attn_pool_bwd(*x[:3], out, lse, x[3], plan, stream=s)))
+    torch.cuda.synchronize()
+    for x, res, w in zip(ins, got, want):
+        for out, lse, grads in res:
+            assert torch.equal(out, w[0]) and torch.equal(lse, w[1])
+            if fused:
+                _check(cu, *x, (out, lse, grads), 300, 5)
+            else:
+                assert all(torch.equal(a, b) for a, b in zip(grads, w[2]))
+    plan.destroy()
+
+
 def test_noalloc_backward_follows_the_plan():
     from paper_2607_23250_b200 import binding as lb
     cu = pools.cu_seqlens([500, 300])
