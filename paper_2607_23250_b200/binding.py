@@ -252,20 +252,20 @@ def _chk_qkv(q, k, v):
     assert q.dtype == k.dtype == v.dtype == torch.bfloat16
     T, hq, d = q.shape
     assert k.shape == v.shape and k.shape[0] == T and k.shape[2] == d, "shapes of q, k and v do not match"
-    assert k.device == v.device == q.device, "tensors on different devices"
+    assert k.get_device() == v.get_device() == q.get_device(), "tensors on different devices"
     return T, hq, d
 
 
 def _given(what, t, n, dtype, like):
     """A tensor of n values that the kernels read or write as a whole."""
-    assert t.dtype is dtype and t.numel() == n, f"{what}: expected {n} values of {dtype}, not {t.numel()} of {t.dtype}"
-    assert t.is_cuda and t.is_contiguous() and t.device == like.device, f"{what}: expected a contiguous tensor on {like.device}"
+    assert (t.dtype is dtype and t.numel() == n and t.is_cuda and t.is_contiguous() and t.get_device() == like.get_device()), \
+        f"{what}: expected {n} contiguous values of {dtype} on {like.device}"
 
 
 def _workspace(workspace, need, like):
     if workspace is None:
         return torch.empty(need, dtype=torch.uint8, device=like.device)
-    assert workspace.is_cuda and workspace.is_contiguous() and workspace.device == like.device
+    assert workspace.is_cuda and workspace.is_contiguous() and workspace.get_device() == like.get_device()
     size = workspace.numel() * workspace.element_size()
     assert size >= need, f"workspace of {size} bytes, the call needs {need}"
     return workspace
@@ -307,8 +307,8 @@ def libra_attn_pool_bwd(q, k, v, out, lse, dout, plan: Plan, dq=None, dk=None, d
     dk = torch.empty_like(k) if dk is None else dk
     dv = torch.empty_like(v) if dv is None else dv
     _chk_bwd(q, k, v, out, lse, dout, dq, dk, dv)
-    workspace = _workspace(workspace, libra_attn_pool_bwd_workspace_bytes(plan, q, k), q)
     dims = _dims(q, k, plan, scale)
+    workspace = _workspace(workspace, int(_lib.libra_attn_pool_bwd_workspace_bytes(plan._h, ctypes.byref(dims))), q)
     _check(_lib.libra_attn_pool_bwd(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), _ptr(dout),
                                     _ptr(plan.cu_seqlens), plan._h, _ptr(dq), _ptr(dk), _ptr(dv), _ptr(workspace),
                                     ctypes.byref(dims), _stream(stream)), "libra_attn_pool_bwd")
