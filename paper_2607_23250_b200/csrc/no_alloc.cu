@@ -52,7 +52,7 @@ extern "C" int libra_attn_pool_bwd_noalloc(const void* q_dev, const void* k_dev,
     if (dims->head_dim != 64 && dims->head_dim != 128 && dims->head_dim != 256) return LIBRA_ERR_UNSUPPORTED;
     size_t need = libra_attn_pool_bwd_workspace_bytes(plan, dims);
     if (need == 0) return LIBRA_ERR_INVALID_ARG;
-    // Partial sums of the sinks' tails are 256 KB a tail and kv head at head_dim 128 (32 / 8 heads, window 1024: 3072 tokens would be the
+    // Partial sums of the sinks' tails are 256 KB a tail and kv head at head_dim 128 (32 / 8 heads, window 1024: some 3000 tokens would be the
     // most).  Beyond that the key-major tiles are walked whole: the same additions in another order, and the tile of a key
     // block that holds sinks as long as its sample (65536 tokens, window 1024, 4 sinks: 22 samples 3.93 ms with the sums, 4.19 without; one
     // sample 4.57 and 5.89).

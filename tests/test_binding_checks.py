@@ -7,9 +7,18 @@ from types import SimpleNamespace
 import pytest
 import torch
 
-from paper_2607_23250_b200 import binding as lb
+lb = None      # the binding, once the library is built
 
 NEED, NEED_CKPT = 1000, 5000       # workspace sizes that the library answers
+
+
+@pytest.fixture(autouse=True, scope="module")
+def binding():
+    global lb
+    from paper_2607_23250_b200 import build
+    build.build()
+    from paper_2607_23250_b200 import binding
+    lb = binding
 
 
 class Dev(torch.Tensor):
